@@ -1,0 +1,475 @@
+"""The paged key/value cache: appending new tokens, attention of new tokens over it, choosing what to keep and
+moving it together.  What is measured, on what, and what each operator computes, in plain torch.
+
+`listed()` are calls of real use, `draw(rng)` gives more over the same ranges, `prepare` makes what a program has
+in hand before a call, `run` is one pass: with `own` through the package's entry points, without it from products,
+sums, exponentials and indexing in 32 bits.  `exact` is the definition in 64 bits, state by state.
+
+Kinds of case
+  append   rotary embedding of new keys, keys and values into pages (fp32, fp16, or int8 with a scale per row)
+  attend   causal or tree-masked attention of new tokens over cached and new keys, grouped heads; with "weights"
+           the attention each cached position received is added to a running sum
+  select   the positions to keep: the first ones, the last ones and the heaviest between
+  compact  the kept rows moved to the front, in place
+
+Heads: those of the package's two encoder shapes and of its small test encoders.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from paper_2604_24273_amd import synth
+
+own = False
+
+HEADS = {"2b": (synth.SHAPE_2B.n_heads, synth.SHAPE_2B.n_kv_heads, synth.SHAPE_2B.head_dim),
+         "3b": (synth.SHAPE_3B.n_heads, synth.SHAPE_3B.n_kv_heads, synth.SHAPE_3B.head_dim),
+         "small_64": (4, 2, 64), "small_32": (8, 8, 32), "small_16": (8, 1, 16)}
+THETA = {"2b": synth.SHAPE_2B.rope_theta}
+DTYPES = {"f32": torch.float32, "f16": torch.float16, "i8": torch.int8}
+SIZE = {"f32": 4, "f16": 2, "i8": 1}
+SMALLEST = 1e-30        # absolute maximum below which an int8 row counts as zeros
+
+
+# ---------------------------------------------------------------- the cases
+
+def _case(name, kind, heads, dtype, states, lo, hi, page, **more):
+    return {"name": name, "kind": kind, "heads": heads, "dtype": dtype, "states": states, "lo": lo, "hi": hi, "page": page,
+            "new_lo": 1, "new_hi": 1, "tree": False, "weights": False, "keep": 0, **more}
+
+
+def listed():
+    return [
+        # one agent, one more token of its episode
+        _case("append_one", "append", "2b", "f32", 1, 200, 200, 32),
+        # the first observations of a batch of episodes
+        _case("append_prompts", "append", "2b", "f16", 32, 0, 0, 64, new_lo=100, new_hi=400),
+        # one agent, one token over a short episode: a call of microseconds
+        _case("attend_one", "attend", "2b", "f32", 1, 300, 300, 32),
+        # vectorised environments, a token each, episodes of very different length
+        _case("attend_64", "attend", "2b", "f16", 64, 500, 3500, 64),
+        # one very long history in the smallest type
+        _case("attend_long", "attend", "2b", "i8", 1, 100000, 100000, 128),
+        # candidate actions tried as branches on one observation: heads of 100, one key head per query head
+        _case("attend_tree", "attend", "3b", "f32", 16, 700, 1500, 32, new_lo=48, new_hi=48, tree=True),
+        # decoding while the weight of each position is summed up
+        _case("attend_weights", "attend", "2b", "f16", 32, 4000, 4200, 64, weights=True),
+        # long documents from the first token
+        _case("attend_prompt", "attend", "2b", "f16", 4, 0, 0, 128, new_lo=4096, new_hi=4096),
+        # every episode over its budget at once
+        _case("select_64", "select", "2b", "f16", 64, 4000, 8000, 64, keep=2048),
+        # one long history, a key head per query head
+        _case("select_long", "select", "3b", "f16", 1, 60000, 60000, 64, keep=8192),
+        _case("compact_64", "compact", "2b", "f16", 64, 4000, 8000, 64, keep=2048),
+        # one episode in full precision
+        _case("compact_one", "compact", "2b", "f32", 1, 3000, 3000, 32, keep=1000),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["append", "attend", "attend", "attend", "attend", "select", "compact"])
+    heads = rng.choice(["2b", "2b", "3b", "small_64", "small_32", "small_16"])
+    hq, hkv, dh = HEADS[heads]
+    c = _case("", kind, heads, rng.choice(["f32", "f16", "i8"]), 0, 0, 0, rng.choice([16, 32, 64, 128, 256]))
+    del c["name"]
+    hi = _log(rng, 8, 60000)
+    most = min(64, max(1, 1_500_000 // (hi * hkv)))
+    c["states"] = _log(rng, 1, most)
+    c["hi"], c["lo"] = hi, rng.randint(hi // 4, hi)
+    if kind in ("append", "attend"):
+        # pairs of a new token and a slot, over all states and query heads: at most those of the largest listed case
+        tokens = min(4096, max(1, 500_000_000 // (c["states"] * (hi + 64) * hq)))
+        c["new_hi"] = rng.choice([1, _log(rng, 1, tokens), _log(rng, 1, tokens)])
+        c["new_lo"] = rng.randint((c["new_hi"] + 1) // 2, c["new_hi"])
+        if kind == "append" and c["dtype"] == "i8":
+            c["states"], c["hi"], c["lo"] = min(c["states"], 8), min(hi, 2000), min(c["lo"], 2000)
+        if kind == "attend":
+            c["tree"] = c["new_hi"] <= 200 and rng.random() < 0.4
+            c["weights"] = rng.random() < 0.3
+    else:
+        c["keep"] = rng.randint(max(1, hi // 8), max(1, hi * 3 // 4))
+    return c
+
+
+# ---------------------------------------------------------------- what a program has in hand
+
+def _row(dh):
+    return (dh + 15) // 16 * 16
+
+
+def _ends(case):
+    """How many first and last positions are always kept."""
+    return min(4, case["keep"] // 4), case["keep"] // 4
+
+
+def _rope_tables(n, dh, theta):
+    inv = torch.pow(torch.tensor(theta, dtype=torch.float64, device="cuda"),
+                    -2.0 * torch.arange(dh // 2, dtype=torch.float64, device="cuda") / dh)
+    a = torch.arange(n, dtype=torch.float64, device="cuda")[:, None] * inv[None, :]
+    return torch.cos(a).float().contiguous(), torch.sin(a).float().contiguous()
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    hq, hkv, dh = HEADS[case["heads"]]
+    n, page, kind = case["states"], case["page"], case["kind"]
+
+    def ints(lo, hi, *shape):
+        return torch.randint(lo, hi + 1, shape, generator=g, device="cuda", dtype=torch.int32)
+
+    def normal(*shape, scale=1.0):
+        return torch.randn(*shape, generator=g, device="cuda") * scale
+
+    def spread(lo, hi):
+        """Lengths evenly from lo to hi, in the seed's order: as many tokens in all whatever the seed."""
+        x = torch.linspace(lo, hi, n, dtype=torch.float64, device="cuda").round().int()
+        return x[torch.randperm(n, generator=g, device="cuda")]
+
+    new = spread(case["new_lo"], case["new_hi"]) if kind in ("append", "attend") else torch.zeros(n, dtype=torch.int32, device="cuda")
+    lens = spread(case["lo"], case["hi"]) + new
+    cu = torch.cat([torch.zeros(1, dtype=torch.int32, device="cuda"), torch.cumsum(new, 0).int()])
+    tokens, max_new = int(cu[-1]), case["new_hi"]
+    max_len = case["hi"] + (max_new if kind in ("append", "attend") else 0)
+    s = {"kind": kind, "heads": (hq, hkv, dh), "page": page, "states": n, "lens": lens, "max_len": max_len}
+    if kind == "select" or kind == "compact" or case["weights"]:
+        # sums of softmax weights: most positions get little, some never any, a few a great deal
+        w = torch.exp(normal(n, hkv, max_len, scale=1.5)) * 0.05
+        w[torch.rand(n, hkv, max_len, generator=g, device="cuda") < 0.2] = 0.0
+        s["weights"] = w
+    if kind != "select":
+        table = -(-max_len // page)
+        pages = n * table + 3
+        # pages in any order, as a program that gives and takes them back ends up with
+        order = torch.randperm(pages, generator=g, device="cuda")[:n * table].int()
+        s["table"] = order.view(n, table).contiguous()
+        row, dtype = _row(dh), DTYPES[case["dtype"]]
+        for name in ("k", "v"):
+            if case["dtype"] == "i8":
+                x = torch.randint(-127, 128, (pages, hkv, page, row), generator=g, device="cuda", dtype=torch.int8)
+                s[name + "_scale"] = (0.7 + 0.6 * torch.rand(pages, hkv, page, generator=g, device="cuda")) * (2.2 / 127)
+            else:
+                x = torch.randn(pages, hkv, page, row, generator=g, device="cuda", dtype=dtype)
+            x[..., dh:] = 0
+            s[name] = x
+    if kind in ("append", "attend"):
+        # positions of the tokens: behind what the state has seen, some of which it may have let go
+        s["cu"], s["max_new"] = cu, max_new
+        gone = ints(0, 50, n) if case["tree"] or case["lo"] > 1000 else torch.zeros_like(lens)
+        state = torch.repeat_interleave(torch.arange(n, device="cuda"), new.long())
+        i = torch.arange(tokens, device="cuda", dtype=torch.int32) - cu[state]
+        base = lens - new
+        if case["tree"]:
+            # each token hangs on an earlier one (or on the history): a token sees its ancestors and itself
+            parent = (torch.rand(n, max_new, generator=g, device="cuda") * (torch.arange(max_new, device="cuda") + 1)).long() - 1
+            sees = torch.zeros(n, max_new + 1, max_new, dtype=torch.bool, device="cuda")    # row 0: the history's end
+            depth = torch.zeros(n, max_new + 1, dtype=torch.int32, device="cuda")
+            rows = torch.arange(n, device="cuda")
+            for t in range(max_new):
+                sees[:, t + 1] = sees[rows, parent[:, t] + 1]
+                sees[:, t + 1, t] = True
+                depth[:, t + 1] = depth[rows, parent[:, t] + 1] + 1
+            words = -(-max_new // 32)
+            bits = torch.zeros(n, max_new, words * 32, dtype=torch.int64, device="cuda")
+            bits[..., :max_new] = sees[:, 1:].long()
+            packed = (bits.view(n, max_new, words, 32) << torch.arange(32, device="cuda")).sum(-1)
+            packed = torch.where(packed >= 1 << 31, packed - (1 << 32), packed).int()
+            s["tree"] = packed[state, i.long()].contiguous()
+            s["positions"] = (base + gone)[state] + depth[state, i.long() + 1] - 1
+        else:
+            s["tree"] = None
+            s["positions"] = (base + gone)[state] + i
+        s["qkv"] = normal(tokens, (hq + 2 * hkv) * dh)
+        s["tokens"] = tokens
+        s["cos"], s["sin"] = _rope_tables(max_len + 64, dh, THETA.get(case["heads"], 10000.0))
+        if kind == "attend":
+            s["out"] = torch.zeros(tokens, hq * dh, device="cuda")
+    if kind in ("select", "compact"):
+        keep = case["keep"]
+        s["first"], s["recent"] = _ends(case)
+        s["keep"] = keep
+        if kind == "compact":
+            # positions picked at random, in order; the first and the last ones among them
+            lot = torch.rand(n, hkv, max_len, generator=g, device="cuda")
+            at = torch.arange(max_len, device="cuda")
+            lot = torch.where(at < s["first"], 2.0, lot)
+            lot = torch.where(at >= (lens - s["recent"])[:, None, None], 2.0, lot)
+            lot = torch.where(at >= lens[:, None, None], -1.0, lot)
+            s["counts"] = torch.clamp(lens, max=keep)
+            kept = torch.sort(torch.topk(lot, min(keep, max_len), dim=-1).indices, dim=-1).values.int()
+            slot = torch.arange(kept.shape[-1], device="cuda", dtype=torch.int32)
+            s["kept"] = torch.where(slot < s["counts"][:, None, None], kept, -1).contiguous()
+        else:
+            s["kept"] = torch.zeros(n, hkv, keep, dtype=torch.int32, device="cuda")
+            s["counts"] = torch.zeros(n, dtype=torch.int32, device="cuda")
+    return s
+
+
+# ---------------------------------------------------------------- one pass
+
+def _own(s):
+    from paper_2604_24273_amd import binding as B
+    from paper_2604_24273_amd import runtime as R
+    hq, hkv, dh = s["heads"]
+    n, kind = s["states"], s["kind"]
+    if kind == "select":
+        B.attention_cache_select(s["weights"], n, hkv, s["lens"], s["max_len"], s["keep"], s["first"], s["recent"], s["kept"],
+                                 s["counts"])
+        return {"kept": s["kept"], "counts": s["counts"]}
+    if "cache" not in s:                 # the handle and the scratch space that a program keeps
+        s["cache"] = B.make_kv_cache(s["k"], s["v"], s.get("k_scale"), s.get("v_scale"), s["table"], dh)
+        if kind == "attend":
+            s["ws"] = R.device_bytes(B.brl_attention_cached_workspace_bytes(s["cache"], hq, s["tokens"], n, s["max_new"],
+                                                                            s["max_len"], "weights" in s))
+    if kind == "append":
+        B.attention_cache_append(s["cache"], s["qkv"], hq, s["tokens"], n, s["cu"], s["max_new"], s["lens"], s["positions"],
+                                 s["cos"], s["sin"])
+        return _held(s)
+    if kind == "attend":
+        B.attention_cached_forward(s["cache"], s["qkv"], hq, s["tokens"], n, s["cu"], s["max_new"], s["lens"], s["max_len"],
+                                   s["positions"], s["cos"], s["sin"], s["tree"], s["out"], s.get("weights"), s["ws"])
+        return {"out": s["out"], "weights": s["weights"]} if "weights" in s else s["out"]
+    B.attention_cache_compact(s["cache"], n, s["lens"], s["max_len"], s["kept"], hkv, None, s["counts"], s["weights"])
+    return _moved(s)
+
+
+def _held(s):
+    """A cache's contents, int8 ones as the values they stand for."""
+    if "k_scale" not in s:
+        return {"k": s["k"], "v": s["v"]}
+    return {"k": s["k"].float() * s["k_scale"][..., None], "v": s["v"].float() * s["v_scale"][..., None]}
+
+
+def _moved(s):
+    """A cache after rows were moved: copies, so int8 codes and their scales as they are."""
+    out = {"k": s["k"], "v": s["v"], "weights": s["weights"]}
+    if "k_scale" in s:
+        out["k_scale"], out["v_scale"] = s["k_scale"], s["v_scale"]
+    return out
+
+
+def _tokens(s):
+    """Of each new token: its state, its index among the state's new ones, its slot."""
+    at = torch.arange(s["tokens"], device="cuda")
+    state = torch.searchsorted(s["cu"], at, right=True, out_int32=True).long() - 1
+    i = at - s["cu"][state]
+    new = s["cu"][1:] - s["cu"][:-1]
+    return state, i, (s["lens"] - new)[state] + i
+
+
+def _rotated(x, cos, sin):
+    """x [tokens, heads, dh] by its tokens' angles: pairs (i, i + dh / 2)."""
+    half = x.shape[-1] // 2
+    a, b, c, d = x[..., :half], x[..., half:], cos[:, None], sin[:, None]
+    return torch.cat([a * c - b * d, b * c + a * d], dim=-1)
+
+
+def _place(s, state, slot):
+    return s["table"][state, slot // s["page"]].long(), slot % s["page"]
+
+
+def _plain_append(s):
+    hq, hkv, dh = s["heads"]
+    rows = s["qkv"].view(s["tokens"], hq + 2 * hkv, dh)
+    pos = s["positions"].long()
+    state, _, slot = _tokens(s)
+    page, off = _place(s, state, slot)
+    new = {"k": _rotated(rows[:, hq:hq + hkv], s["cos"][pos], s["sin"][pos]), "v": rows[:, hq + hkv:]}
+    for name, x in new.items():
+        if s[name].dtype == torch.int8:
+            a = torch.clamp(x.abs().amax(-1), min=SMALLEST)
+            s[name + "_scale"][page, :, off] = a / 127
+            x = torch.clamp(torch.round(x * (127 / a)[..., None]), -127, 127)
+        s[name][page, :, off, :dh] = x.to(s[name].dtype)
+    return _held(s)
+
+
+def _gathered(s, name):
+    """Keys or values of every state in order, [states, kv heads, slots, dh] in 32 bits."""
+    hq, hkv, dh = s["heads"]
+    n, slots = s["states"], s["max_len"]
+    x = s[name][s["table"].long()][..., :dh].float()                    # [states, pages, kv heads, page, dh]
+    if name + "_scale" in s:
+        x = x * s[name + "_scale"][s["table"].long()][..., None]
+    return x.transpose(1, 2).reshape(n, hkv, -1, dh)[:, :, :slots]
+
+
+def _visible(s, state, i, slot):
+    """[states, new, slots]: whether a state's new token sees a slot."""
+    n, new, slots = s["states"], s["max_new"], s["max_len"]
+    at = torch.arange(slots, device="cuda")
+    count = (s["cu"][1:] - s["cu"][:-1])[:, None, None]
+    base = s["lens"][:, None, None] - count
+    if s["tree"] is None:
+        see = at <= base + torch.arange(new, device="cuda")[:, None]
+    else:
+        words = torch.zeros(n, new, s["tree"].shape[1], dtype=torch.int32, device="cuda")
+        words[state, i] = s["tree"]
+        bits = ((words[..., None] >> torch.arange(32, device="cuda")) & 1).flatten(2)
+        j = torch.clamp(at - base, 0, bits.shape[-1] - 1).expand(n, new, slots)
+        see = (at < base) | (torch.gather(bits, 2, j) > 0)
+    return see & (at < s["lens"][:, None, None]) & (torch.arange(new, device="cuda")[:, None] < count)
+
+
+def _plain_attend(s):
+    hq, hkv, dh = s["heads"]
+    n, new, group = s["states"], s["max_new"], hq // hkv
+    state, i, slot = _tokens(s)
+    pos = s["positions"].long()
+    q = torch.zeros(n, new, hq, dh, device="cuda")
+    q[state, i] = _rotated(s["qkv"].view(s["tokens"], -1, dh)[:, :hq], s["cos"][pos], s["sin"][pos])
+    q = q.view(n, new, hkv, group, dh).permute(0, 2, 3, 1, 4).reshape(n, hkv, group * new, dh)
+    x = torch.matmul(q * (1.0 / math.sqrt(dh)), _gathered(s, "k").transpose(2, 3).contiguous())
+    see = _visible(s, state, i, slot)
+    x = x.view(n, hkv, group, new, -1).masked_fill_(~see[:, None, None], -math.inf)
+    top = x.amax(-1, keepdim=True)
+    x = torch.exp(x - torch.where(top == -math.inf, 0.0, top))           # a row that sees nothing: zeros
+    x = x / torch.clamp(x.sum(-1, keepdim=True), min=1e-30)
+    at = torch.arange(s["max_len"], device="cuda")
+    v = torch.where((at < s["lens"][:, None])[:, None, :, None], _gathered(s, "v"), 0.0)
+    y = torch.matmul(x.view(n, hkv, group * new, -1), v).view(n, hkv, group, new, dh)
+    s["out"][:] = y.permute(0, 3, 1, 2, 4).reshape(n, new, hq * dh)[state, i]
+    if "weights" not in s:
+        return s["out"]
+    s["weights"] += x.sum((2, 3))
+    return {"out": s["out"], "weights": s["weights"]}
+
+
+def _plain_select(s):
+    keep, slots = s["keep"], s["max_len"]
+    at = torch.arange(slots, device="cuda")
+    lens = s["lens"][:, None, None]
+    w = torch.where(torch.isnan(s["weights"]), -math.inf, s["weights"])
+    always = (at < s["first"]) | (at >= lens - s["recent"])
+    # three classes in order: always kept, by weight, not there
+    key = torch.where(at >= lens, 2, torch.where(always, 0, 1)).expand(w.shape)
+    order = torch.argsort(w, dim=-1, descending=True, stable=True)
+    order = torch.gather(order, 2, torch.argsort(torch.gather(key, 2, order), dim=-1, stable=True))
+    kept = torch.sort(order[..., :keep], dim=-1).values.int()
+    s["counts"][:] = torch.clamp(s["lens"], max=keep)
+    s["kept"].fill_(-1)
+    s["kept"][..., :kept.shape[-1]] = torch.where(torch.arange(kept.shape[-1], device="cuda") < s["counts"][:, None, None], kept, -1)
+    return {"kept": s["kept"], "counts": s["counts"]}
+
+
+def _plain_compact(s):
+    hkv = s["heads"][1]
+    b, h, i = torch.nonzero(s["kept"] >= 0, as_tuple=True)
+    src = s["kept"][b, h, i].long()
+    page, off = _place(s, b, src)
+    to, at = _place(s, b, i)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        if name in s:
+            s[name][to, h, at] = s[name][page, h, off]
+    s["weights"][b, h, i] = s["weights"][b, h, src]
+    return _moved(s)
+
+
+def run(s):
+    if own:
+        return _own(s)
+    return {"append": _plain_append, "attend": _plain_attend, "select": _plain_select, "compact": _plain_compact}[s["kind"]](s)
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+
+def work(case):
+    hq, hkv, dh = HEADS[case["heads"]]
+    n, kind = case["states"], case["kind"]
+    cached, new = (case["lo"] + case["hi"]) / 2, (case["new_lo"] + case["new_hi"]) / 2
+    row = hkv * (dh * SIZE[case["dtype"]] + (4 if case["dtype"] == "i8" else 0))       # of k or v, one token
+    if kind == "append":
+        return {"bytes": n * new * 2 * (hkv * dh * 4 + row), "flops": n * new * hkv * dh * 3}
+    if kind == "attend":
+        pairs = n * hq * new * (cached + (new + 1) / 2)
+        bytes_ = n * (cached + new) * 2 * row + n * new * hq * dh * 8
+        return {"bytes": bytes_ + (n * (cached + new) * hkv * 8 if case["weights"] else 0), "flops": pairs * 4 * dh}
+    kept = n * hkv * min(case["keep"], cached)
+    if kind == "select":
+        return {"bytes": n * hkv * cached * 4 + kept * 4, "flops": n * hkv * cached}
+    return {"bytes": kept * 4 + 2 * kept * (2 * row / hkv + 4), "flops": 0}
+
+
+# ---------------------------------------------------------------- the definitions, in 64 bits
+
+def exact(case, seed):
+    """State by state and token by token order, nothing shared with the forms above but the inputs."""
+    s = prepare(case, seed)
+    hq, hkv, dh = s["heads"]
+    kind = s["kind"]
+    if kind == "select":
+        return None                      # whole numbers
+    size = s["page"]
+    lens = s["lens"].tolist()
+
+    def rows(name, b, count):
+        """Slots 0 .. count - 1 of state b in 64 bits, [kv heads, count, dh]."""
+        pages = s["table"][b, :-(-count // size)].long()
+        x = s[name][pages].double()
+        if name + "_scale" in s:
+            x = x * s[name + "_scale"][pages].double().unsqueeze(-1)
+        return x.permute(1, 0, 2, 3).flatten(1, 2)[:, :count, :dh]
+
+    if kind == "compact":
+        pools = {name: s[name].double() for name in ("k", "v", "weights", "k_scale", "v_scale") if name in s}
+        for b in range(s["states"]):
+            count = int(s["counts"][b])
+            for h in range(hkv):
+                src = s["kept"][b, h, :count].long()
+                dst = torch.arange(count, device="cuda")
+                t = s["table"][b].long()
+                for name in ("k", "v", "k_scale", "v_scale"):
+                    if name in pools:
+                        pools[name][t[dst // size], h, dst % size] = s[name][t[src // size], h, src % size].double()
+                pools["weights"][b, h, :count] = s["weights"][b, h, src].double()
+        if case["dtype"] == "i8":
+            pools["k"] = pools["v"] = None
+        return pools
+    cu = s["cu"].tolist()
+    cos, sin = s["cos"].double(), s["sin"].double()
+
+    def turned(x, positions):
+        """Each pair as a complex number times exp(i angle)."""
+        z = torch.complex(x[..., :dh // 2], x[..., dh // 2:])
+        p = positions.long()
+        z = z * torch.complex(cos[p], sin[p]).unsqueeze(1)
+        return torch.cat([z.real, z.imag], -1)
+
+    if kind == "append":
+        if case["dtype"] == "i8":
+            return None                  # values on an 8-bit grid
+        pools = {"k": s["k"].double(), "v": s["v"].double()}
+        for b in range(s["states"]):
+            x = s["qkv"][cu[b]:cu[b + 1]].double().view(-1, hq + 2 * hkv, dh)
+            slot = torch.arange(lens[b] - x.shape[0], lens[b], device="cuda")
+            t = s["table"][b].long()
+            pools["k"][t[slot // size], :, slot % size, :dh] = turned(x[:, hq:hq + hkv], s["positions"][cu[b]:cu[b + 1]])
+            pools["v"][t[slot // size], :, slot % size, :dh] = x[:, hq + hkv:]
+        return pools
+    out = torch.zeros(s["tokens"], hq, dh, dtype=torch.float64, device="cuda")
+    total = s["weights"].double() if "weights" in s else None
+    for b in range(s["states"]):
+        m, count = cu[b + 1] - cu[b], lens[b]
+        k, v = rows("k", b, count), rows("v", b, count)
+        q = turned(s["qkv"][cu[b]:cu[b + 1]].double().view(m, -1, dh)[:, :hq], s["positions"][cu[b]:cu[b + 1]])
+        hidden = torch.zeros(m, count, dtype=torch.bool, device="cuda")
+        if s["tree"] is None:
+            hidden[:, count - m:] = torch.ones(m, m, dtype=torch.bool, device="cuda").triu(1)
+        else:
+            j = torch.arange(m, device="cuda")
+            hidden[:, count - m:] = ((s["tree"][cu[b]:cu[b + 1]].long()[:, j // 32] >> (j % 32)) & 1) == 0
+        for h in range(hq):
+            g = h // (hq // hkv)
+            p = torch.softmax((q[:, h] @ k[g].T / math.sqrt(dh)).masked_fill(hidden, -math.inf), -1)
+            p = torch.nan_to_num(p)      # a token that sees nothing
+            out[cu[b]:cu[b + 1], h] = p @ v[g]
+            if total is not None:
+                total[b, g, :count] += p.sum(0)
+    out = out.flatten(1)
+    return out if total is None else {"out": out, "weights": total}
