@@ -284,8 +284,9 @@ def _plain_append(s):
     for name, x in new.items():
         if s[name].dtype == torch.int8:
             a = torch.clamp(x.abs().amax(-1), min=SMALLEST)
-            s[name + "_scale"][page, :, off] = a / 127
-            x = torch.clamp(torch.round(x * (127 / a)[..., None]), -127, 127)
+            most = torch.full_like(a, 127.0)        # (a division by a plain number would be a product with its inverse)
+            s[name + "_scale"][page, :, off] = a / most
+            x = torch.clamp(torch.round(x * (most / a)[..., None]), -127, 127)
         s[name][page, :, off, :dh] = x.to(s[name].dtype)
     return _held(s)
 
