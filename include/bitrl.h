@@ -55,6 +55,10 @@ extern "C" {
 #define BRL_F32   0
 #define BRL_BF16  1    /* widened to fp32 exactly on load */
 
+/* ---- further element types of a key/value cache ---- */
+#define BRL_F16   2
+#define BRL_I8    3    /* codes -127..127, one fp32 scale per row */
+
 /* ---- head activation ---- */
 #define BRL_ACT_TANH 0
 #define BRL_ACT_RELU 1
@@ -338,6 +342,105 @@ int attention_forward(const float* qkv, int B, int S,
                       const int32_t* cu_seqlens /* DEVICE or NULL */, const int32_t* cu_seqlens_host /* HOST or NULL */,
                       int n_heads, int n_kv_heads, int head_dim, float rope_theta, int attn_precision,
                       float* out, void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Paged key/value cache: attention for states whose text grows.  The backbone
+ * f of Sec. 3.1, Eq. 3 is causal, so the rotated keys and the values of a
+ * prefix never change; an agent that keeps them encodes only what an episode
+ * adds.  (The paper encodes every state from its first token and has no cache;
+ * the attention is the one of attention_forward.)
+ *
+ * A cache is a pool of pages.  A page holds page_tokens (16, 32, 64, 128 or
+ * 256) tokens of all k/v heads:
+ *   k, v             [n_pages, n_kv_heads, page_tokens, row] of dtype, row =
+ *                    head_dim rounded up to 16 (append writes zeros behind
+ *                    head_dim; no call computes with what is there)
+ *   k_scale, v_scale [n_pages, n_kv_heads, page_tokens] fp32, BRL_I8 only: a
+ *                    stored value is code * scale
+ *   page_table       DEVICE [B, table_pages] int32: slot j of state b is row
+ *                    j % page_tokens of page page_table[b, j / page_tokens]
+ * dtype BRL_F32 (attention as exact as attention_forward's), BRL_F16 or BRL_I8.
+ * The struct is read on the HOST during the call.  Which pages a state owns
+ * is the caller's business; pages may be shared between states as long as
+ * nobody writes them.  Slots at lens[b] and behind are never read.
+ *
+ * New tokens: qkv [T, (n_heads + 2 n_kv_heads) * head_dim] fp32 rows as in
+ * attention_forward.  State b owns rows cu_new[b] .. cu_new[b+1]-1 (DEVICE [B+1]
+ * int32, at most max_new of them, none is fine; rows behind cu_new[B] are left
+ * alone) or, with cu_new NULL, T / B rows each.  lens DEVICE [B]: the state's
+ * slots in use, the new tokens included; they take the last ones.  positions
+ * DEVICE [T] int32 or NULL (a token's position is its slot); they index the
+ * rotary tables rope_cos, rope_sin DEVICE [rope_len, head_dim / 2] fp32, filled
+ * once by attention_rope_table.
+ *
+ * Device arrays are read on the device only; values outside their range never
+ * lead out of bounds: lens count as at most max_len (which itself must fit the
+ * table) and at least 0, positions are clamped into the table, a page number
+ * outside [0, n_pages) makes its slots disappear (not written, not seen, not
+ * moved), a token that has no slot (more new tokens than lens) sees no key
+ * before slot 0 and is not stored.
+ * All calls only enqueue kernels and can be captured into a HIP graph.
+ *
+ * attention_cache_append: rotates the new keys, stores keys and values.
+ *   fp16: rounded to nearest (|x| < 65504).  int8, per row: a = max(max|x|,
+ *   1e-30), code = clamp(rne(x * (127 / a)), -127, 127), scale = a / 127.
+ *
+ * attention_cached_forward: out [T, n_heads * head_dim] fp32 = softmax(q k^T /
+ *   sqrt(head_dim)) v over the slots that the token sees; query head h reads k/v
+ *   head h / (n_heads / n_kv_heads).  Call it after attention_cache_append.  Without
+ *   tree_mask token i of a state sees its slots up to its own.  With tree_mask
+ *   (DEVICE [T, mask_words] 32-bit words) it sees every slot before the state's
+ *   new tokens, and the state's new token j where bit j % 32 of word j / 32 is
+ *   set (a set bit for itself and for its ancestors: candidate texts as branches of one
+ *   prefix, evaluated together); tokens from 32 * mask_words on are not seen.
+ *   A token that sees nothing gives zeros.  The cache's values within
+ *   |x| < 65504 (BRL_F32: fp16 hi + lo pairs on the matrix cores, as in
+ *   BRL_ATTN_MFMA).
+ *   weights, DEVICE [B, n_kv_heads, ld_weights] or NULL: weights[b, h, j] += sum
+ *   over the state's new tokens and the query heads of k/v head h of the softmax
+ *   weight of slot j, in a fixed order.
+ *
+ * attention_cache_select: which slots to keep.  Where lens[b] > keep: the first
+ *   `first`, the last `recent`, and between them the keep - first - recent with
+ *   the largest weights (of equal ones the lower slot; NaN counts as -inf), for
+ *   each k/v head by itself.  kept [B, n_kv_heads, keep] int32: slots ascending,
+ *   -1 behind the last; counts [B] = min(lens[b], keep).
+ *
+ * attention_cache_compact: row kept[b, h, i] becomes row start[b] + i (0 with
+ *   start NULL) for i < counts[b], in place, k, v, scales and (if given)
+ *   weights.  kept [B, kept_heads, ld_kept], ascending; kept_heads is n_kv_heads
+ *   or 1 (one list for all heads, e.g. the accepted branch of a tree).  Entries
+ *   below start[b] + i or outside the state's slots move nothing.  A state's pages
+ *   must not be shared with another.  The caller sets lens to start + counts.
+ * ------------------------------------------------------------------------ */
+typedef struct brl_kv_cache {
+    int   n_pages, page_tokens, n_kv_heads, head_dim;
+    int   dtype;                        /* BRL_F32, BRL_F16 or BRL_I8 */
+    int   table_pages;                  /* entries of a state's row of the page table */
+    void* k;
+    void* v;
+    float* k_scale;                     /* BRL_I8, else NULL */
+    float* v_scale;
+    const int32_t* page_table;
+} brl_kv_cache;
+
+size_t brl_kv_page_bytes(int page_tokens, int n_kv_heads, int head_dim, int dtype);   /* of k (or v), 0 for bad arguments */
+int attention_rope_table(float* rope_cos, float* rope_sin, int rope_len, int head_dim, float rope_theta, void* stream);
+int attention_cache_append(const brl_kv_cache* cache /* HOST */, const float* qkv, int n_heads, int T, int B,
+                           const int32_t* cu_new, int max_new, const int32_t* lens, const int32_t* positions,
+                           const float* rope_cos, const float* rope_sin, int rope_len, void* stream);
+size_t brl_attention_cached_workspace_bytes(const brl_kv_cache* cache /* HOST */, int n_heads, int T, int B, int max_new,
+                                            int max_len, int want_weights);
+int attention_cached_forward(const brl_kv_cache* cache /* HOST */, const float* qkv, int n_heads, int T, int B,
+                             const int32_t* cu_new, int max_new, const int32_t* lens, int max_len,
+                             const int32_t* positions, const float* rope_cos, const float* rope_sin, int rope_len,
+                             const uint32_t* tree_mask, int mask_words, float* out, float* weights, int ld_weights,
+                             void* workspace, size_t ws_bytes, void* stream);
+int attention_cache_select(const float* weights, int ld_weights, int B, int n_kv_heads, const int32_t* lens, int max_len,
+                           int keep, int first, int recent, int32_t* kept, int32_t* counts, void* stream);
+int attention_cache_compact(const brl_kv_cache* cache /* HOST */, int B, const int32_t* lens, int max_len,
+                            const int32_t* kept, int kept_heads, int ld_kept, const int32_t* start,
+                            const int32_t* counts, float* weights, int ld_weights, void* stream);
 
 /* ------------------------------------------------------------------------
  * State-to-token front end: serialize(s_t) of Sec. 3.1, Eq. 3 ("converts

@@ -17,7 +17,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libbitrl.so")
 
 BRL_OK, BRL_EINVAL, BRL_ENOSPC, BRL_EHIP = 0, 1, 2, 3
-BRL_F32, BRL_BF16 = 0, 1
+BRL_F32, BRL_BF16, BRL_F16, BRL_I8 = 0, 1, 2, 3
 BRL_ACT_TANH, BRL_ACT_RELU = 0, 1
 BRL_ATTN_F32, BRL_ATTN_MFMA = 0, 1
 BRL_W_TERNARY, BRL_W_INT8 = 0, 1
@@ -77,6 +77,13 @@ class brl_ppo_config(C.Structure):
                 ("normalize_adv", c_int)]
 
 
+class brl_kv_cache(C.Structure):
+    _fields_ = [("n_pages", c_int), ("page_tokens", c_int), ("n_kv_heads", c_int), ("head_dim", c_int),
+                ("dtype", c_int), ("table_pages", c_int),
+                ("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p),
+                ("page_table", c_void_p)]
+
+
 _SIGNATURES = {
     "brl_last_error": (C.c_char_p, []),
     "brl_abi_version": (c_int, []),
@@ -113,6 +120,18 @@ _SIGNATURES = {
     "brl_attention_workspace_bytes": (c_size_t, [c_int, c_int, c_int, c_int, c_int]),
     "attention_forward": (c_int, [c_void_p, c_int, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_float, c_int,
                                   c_void_p, c_void_p, c_size_t, c_void_p]),
+    "brl_kv_page_bytes": (c_size_t, [c_int, c_int, c_int, c_int]),
+    "attention_rope_table": (c_int, [c_void_p, c_void_p, c_int, c_int, c_float, c_void_p]),
+    "attention_cache_append": (c_int, [C.POINTER(brl_kv_cache), c_void_p, c_int, c_int, c_int, c_void_p, c_int, c_void_p,
+                                       c_void_p, c_void_p, c_void_p, c_int, c_void_p]),
+    "brl_attention_cached_workspace_bytes": (c_size_t, [C.POINTER(brl_kv_cache), c_int, c_int, c_int, c_int, c_int, c_int]),
+    "attention_cached_forward": (c_int, [C.POINTER(brl_kv_cache), c_void_p, c_int, c_int, c_int, c_void_p, c_int, c_void_p,
+                                         c_int, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p,
+                                         c_int, c_void_p, c_size_t, c_void_p]),
+    "attention_cache_select": (c_int, [c_void_p, c_int, c_int, c_int, c_void_p, c_int, c_int, c_int, c_int, c_void_p,
+                                       c_void_p, c_void_p]),
+    "attention_cache_compact": (c_int, [C.POINTER(brl_kv_cache), c_int, c_void_p, c_int, c_void_p, c_int, c_int, c_void_p,
+                                        c_void_p, c_void_p, c_int, c_void_p]),
     "brl_serialize_text": (c_size_t, [c_void_p, c_int, C.c_char_p, c_size_t]),
     "brl_tokenize": (c_int, [C.c_char_p, c_size_t, c_void_p, c_int, C.POINTER(c_int)]),
     "serialize_states": (c_int, [c_void_p, c_int, c_int, c_int, c_void_p, c_void_p]),
@@ -307,6 +326,78 @@ def attention_forward(qkv: torch.Tensor, B: int, S: int, cu_seqlens: Optional[to
                                    None if cu_seqlens_host is None else cu_seqlens_host.ctypes.data,
                                    n_heads, n_kv_heads, head_dim, rope_theta, attn_precision, _ptr(out), _ptr(workspace),
                                    workspace.numel() * workspace.element_size(), _stream()))
+
+
+# -- paged key/value cache
+
+_KV_TORCH = {torch.float32: BRL_F32, torch.float16: BRL_F16, torch.int8: BRL_I8}
+
+
+def make_kv_cache(k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor], v_scale: Optional[torch.Tensor],
+                  page_table: torch.Tensor, head_dim: int) -> brl_kv_cache:
+    """k, v: [n_pages, n_kv_heads, page_tokens, row] with row = head_dim rounded up to 16, float32, float16 or int8; scales
+    (int8 only): float32 [n_pages, n_kv_heads, page_tokens]; page_table: int32 [states, table_pages].  The tensors must
+    outlive the struct."""
+    if k.dtype not in _KV_TORCH or v.dtype != k.dtype or v.shape != k.shape or k.dim() != 4:
+        raise ValueError("k and v must be float32, float16 or int8 tensors of one shape [pages, kv heads, page tokens, row]")
+    if k.shape[3] != (head_dim + 15) // 16 * 16:
+        raise ValueError("rows of a cache hold head_dim rounded up to 16 elements")
+    for s in (k_scale, v_scale):
+        if s is not None and (s.dtype != torch.float32 or s.shape != k.shape[:3]):
+            raise ValueError("scales must be float32 [pages, kv heads, page tokens]")
+    if page_table.dtype != torch.int32 or page_table.dim() != 2:
+        raise ValueError("page_table must be int32 [states, pages]")
+    return brl_kv_cache(k.shape[0], k.shape[2], k.shape[1], head_dim, _KV_TORCH[k.dtype], page_table.shape[1],
+                        _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(page_table))
+
+
+def brl_kv_page_bytes(page_tokens: int, n_kv_heads: int, head_dim: int, dtype: int) -> int:
+    return lib().brl_kv_page_bytes(page_tokens, n_kv_heads, head_dim, dtype)
+
+
+def attention_rope_table(rope_cos: torch.Tensor, rope_sin: torch.Tensor, head_dim: int, rope_theta: float) -> None:
+    """rope_cos, rope_sin: float32 [rope_len, head_dim / 2]."""
+    _check(lib().attention_rope_table(_ptr(rope_cos), _ptr(rope_sin), rope_cos.shape[0], head_dim, rope_theta, _stream()))
+
+
+def attention_cache_append(cache: brl_kv_cache, qkv: torch.Tensor, n_heads: int, T: int, B: int,
+                           cu_new: Optional[torch.Tensor], max_new: int, lens: torch.Tensor,
+                           positions: Optional[torch.Tensor], rope_cos: torch.Tensor, rope_sin: torch.Tensor) -> None:
+    """cu_new [B + 1], lens [B], positions [T]: int32 device tensors (cu_new and positions may be None)."""
+    _check(lib().attention_cache_append(C.byref(cache), _ptr(qkv), n_heads, T, B, _ptr(cu_new), max_new, _ptr(lens),
+                                        _ptr(positions), _ptr(rope_cos), _ptr(rope_sin), rope_cos.shape[0], _stream()))
+
+
+def brl_attention_cached_workspace_bytes(cache: brl_kv_cache, n_heads: int, T: int, B: int, max_new: int, max_len: int,
+                                         want_weights: bool) -> int:
+    return lib().brl_attention_cached_workspace_bytes(C.byref(cache), n_heads, T, B, max_new, max_len, 1 if want_weights else 0)
+
+
+def attention_cached_forward(cache: brl_kv_cache, qkv: torch.Tensor, n_heads: int, T: int, B: int,
+                             cu_new: Optional[torch.Tensor], max_new: int, lens: torch.Tensor, max_len: int,
+                             positions: Optional[torch.Tensor], rope_cos: torch.Tensor, rope_sin: torch.Tensor,
+                             tree_mask: Optional[torch.Tensor], out: torch.Tensor, weights: Optional[torch.Tensor],
+                             workspace: torch.Tensor) -> None:
+    """tree_mask: int32 [T, words] (bit patterns) or None; weights: float32 [B, n_kv_heads, slots] or None."""
+    _check(lib().attention_cached_forward(C.byref(cache), _ptr(qkv), n_heads, T, B, _ptr(cu_new), max_new, _ptr(lens), max_len,
+                                          _ptr(positions), _ptr(rope_cos), _ptr(rope_sin), rope_cos.shape[0], _ptr(tree_mask),
+                                          0 if tree_mask is None else tree_mask.shape[1], _ptr(out), _ptr(weights),
+                                          0 if weights is None else weights.shape[-1], _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(), _stream()))
+
+
+def attention_cache_select(weights: torch.Tensor, B: int, n_kv_heads: int, lens: torch.Tensor, max_len: int, keep: int,
+                           first: int, recent: int, kept: torch.Tensor, counts: torch.Tensor) -> None:
+    """weights: float32 [B, n_kv_heads, slots]; kept: int32 [B, n_kv_heads, keep]; counts: int32 [B]."""
+    _check(lib().attention_cache_select(_ptr(weights), weights.shape[-1], B, n_kv_heads, _ptr(lens), max_len, keep, first, recent,
+                                        _ptr(kept), _ptr(counts), _stream()))
+
+
+def attention_cache_compact(cache: brl_kv_cache, B: int, lens: torch.Tensor, max_len: int, kept: torch.Tensor, kept_heads: int,
+                            start: Optional[torch.Tensor], counts: torch.Tensor, weights: Optional[torch.Tensor]) -> None:
+    """kept: int32 [B, kept_heads, entries]; start (or None) and counts: int32 [B]."""
+    _check(lib().attention_cache_compact(C.byref(cache), B, _ptr(lens), max_len, _ptr(kept), kept_heads, kept.shape[-1], _ptr(start),
+                                         _ptr(counts), _ptr(weights), 0 if weights is None else weights.shape[-1], _stream()))
 
 
 BRL_SERIALIZE_VOCAB = 457

@@ -962,6 +962,150 @@ int attention_forward(const float* qkv, int B, int S, const int32_t* cu_seqlens,
     return launch_attention_f32(qkv, ld, B, S, sm, n_heads, n_kv_heads, head_dim, cos_t, sin_t, out, s);
 }
 
+namespace {
+
+bool kv_shape_ok(int page_tokens, int n_kv_heads, int head_dim, int dtype) {
+    return page_tokens >= 16 && page_tokens <= 256 && (page_tokens & (page_tokens - 1)) == 0 && n_kv_heads >= 1 && n_kv_heads <= 4096 &&
+           (head_dim == 16 || head_dim == 32 || head_dim == 64 || head_dim == 100 || head_dim == 128) &&
+           (dtype == BRL_F32 || dtype == BRL_F16 || dtype == BRL_I8);
+}
+
+constexpr int KV_MAX_TOKENS = 1 << 28;               // new tokens of a call and slots of a state: products with head counts fit
+
+int view_cache(const brl_kv_cache* c, const char* who, KvView& v) {
+    BRL_REQUIRE(c != nullptr, "%s: null cache", who);
+    BRL_REQUIRE(kv_shape_ok(c->page_tokens, c->n_kv_heads, c->head_dim, c->dtype),
+                "%s: bad cache (page_tokens %d, n_kv_heads %d, head_dim %d not in {16, 32, 64, 100, 128}, dtype %d)", who,
+                c->page_tokens, c->n_kv_heads, c->head_dim, c->dtype);
+    BRL_REQUIRE(c->n_pages >= 1 && c->table_pages >= 1 && c->table_pages <= KV_MAX_TOKENS / c->page_tokens,
+                "%s: n_pages = %d, table_pages = %d", who, c->n_pages, c->table_pages);
+    BRL_REQUIRE(c->k && c->v && c->page_table && aligned16(c->k) && aligned16(c->v), "%s: null or misaligned pointer in brl_kv_cache", who);
+    BRL_REQUIRE((c->dtype == BRL_I8) == (c->k_scale != nullptr) && (c->dtype == BRL_I8) == (c->v_scale != nullptr),
+                "%s: an int8 cache needs k_scale and v_scale, any other has none", who);
+    v.k = static_cast<char*>(c->k); v.v = static_cast<char*>(c->v);
+    v.ks = c->k_scale; v.vs = c->v_scale;
+    v.table = c->page_table;
+    v.n_pages = c->n_pages; v.n_kv = c->n_kv_heads; v.dh = c->head_dim; v.row = kv_row(c->head_dim);
+    v.dtype = c->dtype; v.table_pages = c->table_pages;
+    v.page_shift = __builtin_ctz((unsigned)c->page_tokens);
+    return BRL_OK;
+}
+
+bool head_counts_ok(int n_heads, int n_kv_heads) { return n_heads >= n_kv_heads && n_heads <= 4096 && n_heads % n_kv_heads == 0; }
+
+int check_new_tokens(const KvView& v, const float* qkv, int n_heads, int T, int B, const int32_t* cu_new, int max_new, const int32_t* lens,
+                     const int32_t* positions, const float* rope_cos, const float* rope_sin, int rope_len, const char* who, NewTokens& t) {
+    BRL_REQUIRE(qkv && lens && rope_cos && rope_sin && aligned16(qkv) && aligned16(rope_cos) && aligned16(rope_sin),
+                "%s: null or misaligned pointer", who);
+    BRL_REQUIRE(head_counts_ok(n_heads, v.n_kv), "%s: n_heads %d not a multiple of n_kv_heads %d", who, n_heads, v.n_kv);
+    BRL_REQUIRE(T >= 1 && T <= KV_MAX_TOKENS && B >= 1 && max_new >= 1 && max_new <= T, "%s: T = %d, B = %d, max_new = %d", who, T, B, max_new);
+    BRL_REQUIRE(cu_new || (T % B == 0 && T / B == max_new), "%s: without cu_new every state has max_new = T / B tokens (T %d, B %d, max_new %d)",
+                who, T, B, max_new);
+    BRL_REQUIRE(rope_len >= 1, "%s: rope_len = %d", who, rope_len);
+    // workgroups and items of a launch are counted in 32 bits
+    BRL_REQUIRE((long long)max_new * n_heads * B <= (1ll << 30) && (long long)B * n_heads <= (1 << 22),
+                "%s: too much for one call (max_new %d, B %d, n_heads %d)", who, max_new, B, n_heads);
+    t.cu = cu_new; t.lens = lens; t.pos = positions;
+    t.cos_t = rope_cos; t.sin_t = rope_sin;
+    t.T = T; t.B = B; t.max_new = max_new; t.max_len = v.table_pages << v.page_shift; t.rope_len = rope_len;
+    return BRL_OK;
+}
+
+}  // namespace
+
+size_t brl_kv_page_bytes(int page_tokens, int n_kv_heads, int head_dim, int dtype) {
+    if (!kv_shape_ok(page_tokens, n_kv_heads, head_dim, dtype)) return 0;
+    return (size_t)page_tokens * n_kv_heads * kv_row(head_dim) * kv_bytes(dtype);
+}
+
+int attention_rope_table(float* rope_cos, float* rope_sin, int rope_len, int head_dim, float rope_theta, void* stream) {
+    BRL_REQUIRE(rope_cos && rope_sin && aligned16(rope_cos) && aligned16(rope_sin), "attention_rope_table: null or misaligned pointer");
+    BRL_REQUIRE(rope_len >= 1 && rope_len <= (1 << 24) && head_dim >= 2 && head_dim <= 128 && head_dim % 2 == 0,
+                "attention_rope_table: rope_len = %d, head_dim = %d", rope_len, head_dim);
+    BRL_REQUIRE(rope_theta > 0.f, "attention_rope_table: rope_theta must be positive");
+    return launch_rope_table(rope_cos, rope_sin, rope_len, head_dim, rope_theta, static_cast<hipStream_t>(stream));
+}
+
+int attention_cache_append(const brl_kv_cache* cache, const float* qkv, int n_heads, int T, int B, const int32_t* cu_new, int max_new,
+                           const int32_t* lens, const int32_t* positions, const float* rope_cos, const float* rope_sin, int rope_len,
+                           void* stream) {
+    KvView v;
+    NewTokens t;
+    if (int rc = view_cache(cache, "attention_cache_append", v)) return rc;
+    if (int rc = check_new_tokens(v, qkv, n_heads, T, B, cu_new, max_new, lens, positions, rope_cos, rope_sin, rope_len,
+                                  "attention_cache_append", t))
+        return rc;
+    return launch_cache_append(v, t, qkv, n_heads, static_cast<hipStream_t>(stream));
+}
+
+size_t brl_attention_cached_workspace_bytes(const brl_kv_cache* c, int n_heads, int T, int B, int max_new, int max_len, int want_weights) {
+    if (!c || !kv_shape_ok(c->page_tokens, c->n_kv_heads, c->head_dim, c->dtype) || !head_counts_ok(n_heads, c->n_kv_heads) || T < 1 ||
+        T > KV_MAX_TOKENS || B < 1 || max_new < 1 || max_new > T || max_len < 1 || max_len > KV_MAX_TOKENS)
+        return 0;
+    KvView v;
+    memset(&v, 0, sizeof(v));
+    v.n_kv = c->n_kv_heads; v.dh = c->head_dim; v.row = kv_row(c->head_dim); v.dtype = c->dtype;
+    v.page_shift = __builtin_ctz((unsigned)c->page_tokens);
+    const size_t need = cached_attention_ws_bytes(v, n_heads, T, B, max_new, max_len, want_weights != 0);
+    return round_up_sz(need ? need : 1, ALIGN);
+}
+
+int attention_cached_forward(const brl_kv_cache* cache, const float* qkv, int n_heads, int T, int B, const int32_t* cu_new, int max_new,
+                             const int32_t* lens, int max_len, const int32_t* positions, const float* rope_cos, const float* rope_sin,
+                             int rope_len, const uint32_t* tree_mask, int mask_words, float* out, float* weights, int ld_weights,
+                             void* workspace, size_t ws_bytes, void* stream) {
+    const char* who = "attention_cached_forward";
+    CachedAttention a;
+    if (int rc = view_cache(cache, who, a.c)) return rc;
+    if (int rc = check_new_tokens(a.c, qkv, n_heads, T, B, cu_new, max_new, lens, positions, rope_cos, rope_sin, rope_len, who, a.t)) return rc;
+    BRL_REQUIRE(out && workspace && aligned16(out) && aligned16(workspace), "%s: null or misaligned pointer", who);
+    BRL_REQUIRE(max_len >= 1 && max_len <= a.t.max_len, "%s: max_len = %d, a row of the page table holds %d", who, max_len, a.t.max_len);
+    BRL_REQUIRE((tree_mask == nullptr) == (mask_words == 0) && mask_words >= 0 && mask_words <= KV_MAX_TOKENS / 32,
+                "%s: mask_words = %d", who, mask_words);
+    BRL_REQUIRE(!weights || ld_weights >= max_len, "%s: ld_weights = %d below max_len = %d", who, ld_weights, max_len);
+    const size_t need = brl_attention_cached_workspace_bytes(cache, n_heads, T, B, max_new, max_len, weights != nullptr);
+    if (ws_bytes < need) {
+        set_error("%s: workspace %zu < %zu", who, ws_bytes, need);
+        return BRL_ENOSPC;
+    }
+    a.t.max_len = max_len;
+    a.qkv = qkv; a.n_heads = n_heads;
+    a.tree = tree_mask; a.mask_words = mask_words;
+    a.out = out; a.weights = weights; a.ld_weights = (size_t)ld_weights;
+    return launch_cached_attention(a, workspace, static_cast<hipStream_t>(stream));
+}
+
+int attention_cache_select(const float* weights, int ld_weights, int B, int n_kv_heads, const int32_t* lens, int max_len, int keep, int first,
+                           int recent, int32_t* kept, int32_t* counts, void* stream) {
+    const char* who = "attention_cache_select";
+    BRL_REQUIRE(weights && lens && kept && counts, "%s: null pointer", who);
+    BRL_REQUIRE(B >= 1 && n_kv_heads >= 1 && (long long)B * n_kv_heads <= (1 << 21), "%s: B = %d, n_kv_heads = %d", who, B, n_kv_heads);
+    BRL_REQUIRE(max_len >= 1 && max_len <= KV_MAX_TOKENS && ld_weights >= max_len, "%s: max_len = %d, ld_weights = %d", who, max_len, ld_weights);
+    BRL_REQUIRE(first >= 0 && recent >= 0 && keep >= 1 && keep <= KV_MAX_TOKENS && (long long)first + recent <= keep,
+                "%s: keep = %d must be positive and hold first = %d and recent = %d", who, keep, first, recent);
+    return launch_cache_select(weights, (size_t)ld_weights, B, n_kv_heads, lens, max_len, keep, first, recent, kept, counts,
+                               static_cast<hipStream_t>(stream));
+}
+
+int attention_cache_compact(const brl_kv_cache* cache, int B, const int32_t* lens, int max_len, const int32_t* kept, int kept_heads,
+                            int ld_kept, const int32_t* start, const int32_t* counts, float* weights, int ld_weights, void* stream) {
+    const char* who = "attention_cache_compact";
+    CompactArgs a;
+    if (int rc = view_cache(cache, who, a.c)) return rc;
+    BRL_REQUIRE(lens && kept && counts, "%s: null pointer", who);
+    BRL_REQUIRE(B >= 1 && (long long)B * a.c.n_kv <= (1 << 18), "%s: B = %d, n_kv_heads = %d", who, B, a.c.n_kv);
+    BRL_REQUIRE(max_len >= 1 && max_len <= (a.c.table_pages << a.c.page_shift), "%s: max_len = %d, a row of the page table holds %d", who,
+                max_len, a.c.table_pages << a.c.page_shift);
+    BRL_REQUIRE(kept_heads == 1 || kept_heads == a.c.n_kv, "%s: kept_heads = %d is neither 1 nor n_kv_heads = %d", who, kept_heads, a.c.n_kv);
+    BRL_REQUIRE(ld_kept >= 1, "%s: ld_kept = %d", who, ld_kept);
+    BRL_REQUIRE(!weights || ld_weights >= max_len, "%s: ld_weights = %d below max_len = %d", who, ld_weights, max_len);
+    a.lens = lens; a.B = B; a.max_len = max_len;
+    a.kept = kept; a.kept_heads = kept_heads; a.ld_kept = ld_kept;
+    a.start = start; a.counts = counts;
+    a.weights = weights; a.ld_weights = (size_t)ld_weights;
+    return launch_cache_compact(a, static_cast<hipStream_t>(stream));
+}
+
 size_t brl_head_workspace_bytes(const brl_head* head, int B) {
     if (!head || B < 1) return 0;
     if (!mlp_sized(&head->policy) || !mlp_sized(&head->value)) return 0;

@@ -237,6 +237,83 @@ int launch_embed(const uint16_t* table, const int32_t* ids, int M, int d, int vo
 // M rows in all; lengths (or nullptr) applies to the uniform layout only
 int launch_final_pool(const float* x, const float* gain, int B, int S, int M, int d, const int32_t* lengths,
                       const SeqMap& sm, float eps_norm, float* rinv, float* h, hipStream_t s);
+// ---- paged key/value cache ----
+// A row (one token of one k/v head) is kv_row(head_dim) elements, zeros behind head_dim, so that every row of every type
+// starts on 16 bytes; a page of one head is page_tokens rows back to back.
+__host__ __device__ inline int kv_row(int head_dim) { return (head_dim + 15) / 16 * 16; }
+__host__ __device__ inline int kv_bytes(int dtype) { return dtype == BRL_F32 ? 4 : dtype == BRL_F16 ? 2 : 1; }
+struct KvView {
+    char *k, *v;              // [n_pages][n_kv][1 << page_shift][row] of dtype
+    float *ks, *vs;           // [n_pages][n_kv][1 << page_shift], BRL_I8 only
+    const int32_t* table;     // [states][table_pages]
+    int n_pages, page_shift, n_kv, dh, row, dtype, table_pages;
+};
+// Index of a slot's row in units of rows, -1 for a page number outside the pool: nothing is read or written there.
+__device__ __forceinline__ long long kv_row_index(const KvView& c, int b, int h, int slot) {
+    const int page = c.table[(size_t)b * c.table_pages + (slot >> c.page_shift)];
+    if ((unsigned)page >= (unsigned)c.n_pages) return -1;
+    return (((long long)page * c.n_kv + h) << c.page_shift) + (slot & ((1 << c.page_shift) - 1));
+}
+// New tokens of the states of a call: rows row0 .. row0 + n - 1 of state b, in the slots base .. base + n - 1 of its cache.
+// Whatever the device arrays hold, rows stay inside [0, T) and slots inside the table (base may be negative: such tokens
+// have no slot).
+struct NewTokens {
+    const int32_t* cu;        // [B + 1] or nullptr: every state has T / B
+    const int32_t* lens;      // [B] slots in use, the new ones included
+    const int32_t* pos;       // [T] positions or nullptr: a token's slot
+    const float *cos_t, *sin_t;
+    int T, B, max_new, max_len, rope_len;
+};
+struct StateTokens {
+    int row0, n, len, base;
+};
+__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+__device__ __forceinline__ StateTokens state_tokens(const NewTokens& t, const KvView& c, int b) {
+    StateTokens s;
+    if (t.cu) {
+        s.row0 = clampi(t.cu[b], 0, t.T);
+        s.n = clampi(t.cu[b + 1], s.row0, t.T) - s.row0;
+        if (s.n > t.max_new) s.n = t.max_new;
+    } else {
+        s.n = t.T / t.B;
+        s.row0 = b * s.n;
+    }
+    s.len = clampi(t.lens[b], 0, t.max_len);
+    s.base = s.len - s.n;
+    return s;
+}
+__device__ __forceinline__ int rope_position(const NewTokens& t, int row, int slot) {
+    return clampi(t.pos ? t.pos[row] : slot, 0, t.rope_len - 1);
+}
+int launch_cache_append(const KvView& c, const NewTokens& t, const float* qkv, int n_heads, hipStream_t s);
+struct CachedAttention {
+    KvView c;
+    NewTokens t;
+    const float* qkv;         // [T, (n_heads + 2 n_kv) dh]
+    int n_heads;
+    const uint32_t* tree;     // [T, mask_words] or nullptr: causal
+    int mask_words;
+    float* out;               // [T, n_heads dh]
+    float* weights;           // [B, n_kv, ld_weights] or nullptr
+    size_t ld_weights;
+};
+size_t cached_attention_ws_bytes(const KvView& c, int n_heads, int T, int B, int max_new, int max_len, bool weights);
+int launch_cached_attention(const CachedAttention& a, void* workspace, hipStream_t s);
+int launch_cache_select(const float* weights, size_t ld_weights, int B, int n_kv, const int32_t* lens, int max_len, int keep,
+                        int first, int recent, int32_t* kept, int32_t* counts, hipStream_t s);
+struct CompactArgs {
+    KvView c;
+    const int32_t* lens;      // [B]
+    int B, max_len;
+    const int32_t* kept;      // [B, kept_heads, ld_kept]
+    int kept_heads, ld_kept;
+    const int32_t* start;     // [B] or nullptr: 0
+    const int32_t* counts;    // [B]
+    float* weights;           // [B, n_kv, ld_weights] or nullptr
+    size_t ld_weights;
+};
+int launch_cache_compact(const CompactArgs& a, hipStream_t s);
+
 // fp32 MLP heads evaluated together on the same h: policy and value, or an ensemble of value heads
 constexpr int MAX_HEADS = 8;
 constexpr int MAX_MLP_LAYERS = 8;
