@@ -998,10 +998,11 @@ int check_new_tokens(const KvView& v, const float* qkv, int n_heads, int T, int 
     BRL_REQUIRE(qkv && lens && rope_cos && rope_sin && aligned16(qkv) && aligned16(rope_cos) && aligned16(rope_sin),
                 "%s: null or misaligned pointer", who);
     BRL_REQUIRE(head_counts_ok(n_heads, v.n_kv), "%s: n_heads %d not a multiple of n_kv_heads %d", who, n_heads, v.n_kv);
-    BRL_REQUIRE(T >= 1 && T <= KV_MAX_TOKENS && B >= 1 && max_new >= 1 && max_new <= T, "%s: T = %d, B = %d, max_new = %d", who, T, B, max_new);
+    BRL_REQUIRE(T >= 1 && T <= KV_MAX_TOKENS && B >= 1 && max_new >= 1, "%s: T = %d, B = %d, max_new = %d", who, T, B, max_new);
     BRL_REQUIRE(cu_new || (T % B == 0 && T / B == max_new), "%s: without cu_new every state has max_new = T / B tokens (T %d, B %d, max_new %d)",
                 who, T, B, max_new);
     BRL_REQUIRE(rope_len >= 1, "%s: rope_len = %d", who, rope_len);
+    if (max_new > T) max_new = T;
     // workgroups and items of a launch are counted in 32 bits
     BRL_REQUIRE((long long)max_new * n_heads * B <= (1ll << 30) && (long long)B * n_heads <= (1 << 22),
                 "%s: too much for one call (max_new %d, B %d, n_heads %d)", who, max_new, B, n_heads);
@@ -1040,8 +1041,9 @@ int attention_cache_append(const brl_kv_cache* cache, const float* qkv, int n_he
 
 size_t brl_attention_cached_workspace_bytes(const brl_kv_cache* c, int n_heads, int T, int B, int max_new, int max_len, int want_weights) {
     if (!c || !kv_shape_ok(c->page_tokens, c->n_kv_heads, c->head_dim, c->dtype) || !head_counts_ok(n_heads, c->n_kv_heads) || T < 1 ||
-        T > KV_MAX_TOKENS || B < 1 || max_new < 1 || max_new > T || max_len < 1 || max_len > KV_MAX_TOKENS)
+        T > KV_MAX_TOKENS || B < 1 || max_new < 1 || max_len < 1 || max_len > KV_MAX_TOKENS)
         return 0;
+    if (max_new > T) max_new = T;
     KvView v;
     memset(&v, 0, sizeof(v));
     v.n_kv = c->n_kv_heads; v.dh = c->head_dim; v.row = kv_row(c->head_dim); v.dtype = c->dtype;

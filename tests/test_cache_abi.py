@@ -33,8 +33,9 @@ def test_sizes(B):
     assert C.sizeof(B.brl_kv_cache) == 6 * 4 + 5 * C.sizeof(C.c_void_p)
     need = lambda *a: B.brl_attention_cached_workspace_bytes(cache(B), *a)  # noqa: E731
     assert need(4, 8, 8, 1, 128, True) > 0
-    for bad in ((3, 8, 8, 1, 128), (4, 0, 8, 1, 128), (4, 8, 0, 1, 128), (4, 8, 8, 0, 128), (4, 8, 8, 9, 128), (4, 8, 8, 1, 0)):
+    for bad in ((3, 8, 8, 1, 128), (4, 0, 8, 1, 128), (4, 8, 0, 1, 128), (4, 8, 8, 0, 128), (4, 8, 8, 1, 0)):
         assert need(*bad, False) == 0
+    assert need(4, 8, 8, 9, 128, True) == need(4, 8, 8, 8, 128, True)             # a bound past the tokens of the call
     assert B.brl_attention_cached_workspace_bytes(cache(B, head_dim=80), 4, 8, 8, 1, 128, False) == 0
 
 
