@@ -359,6 +359,7 @@ int attention_forward(const float* qkv, int B, int S,
  *                    stored value is code * scale
  *   page_table       DEVICE [B, table_pages] int32: slot j of state b is row
  *                    j % page_tokens of page page_table[b, j / page_tokens]
+ * (n_pages * n_kv_heads * page_tokens below 2^31.)
  * dtype BRL_F32 (attention as exact as attention_forward's), BRL_F16 or BRL_I8.
  * The struct is read on the HOST during the call.  Which pages a state owns
  * is the caller's business; pages may be shared between states as long as

@@ -979,6 +979,8 @@ int view_cache(const brl_kv_cache* c, const char* who, KvView& v) {
                 c->page_tokens, c->n_kv_heads, c->head_dim, c->dtype);
     BRL_REQUIRE(c->n_pages >= 1 && c->table_pages >= 1 && c->table_pages <= KV_MAX_TOKENS / c->page_tokens,
                 "%s: n_pages = %d, table_pages = %d", who, c->n_pages, c->table_pages);
+    BRL_REQUIRE((long long)c->n_pages * c->n_kv_heads * c->page_tokens < (1ll << 31),
+                "%s: %d pages of %d heads and %d tokens are 2^31 rows or more", who, c->n_pages, c->n_kv_heads, c->page_tokens);
     BRL_REQUIRE(c->k && c->v && c->page_table && aligned16(c->k) && aligned16(c->v), "%s: null or misaligned pointer in brl_kv_cache", who);
     BRL_REQUIRE((c->dtype == BRL_I8) == (c->k_scale != nullptr) && (c->dtype == BRL_I8) == (c->v_scale != nullptr),
                 "%s: an int8 cache needs k_scale and v_scale, any other has none", who);

@@ -76,10 +76,8 @@ __device__ __forceinline__ int lds_chunk(int key, int c) {
     return key * S::LS + ((c ^ f) << 4);
 }
 
-// ---- a state's block of 32 slots: where its two halves of 16 lie (pages hold 16 at least) ----
-struct Block {
-    long long lo, hi;         // rows of the pool, -1: not there
-};
+// A block of 32 slots lies in two halves of 16 (pages hold 16 at least): lo and hi are their first rows in the pool, -1 where
+// there is none.
 
 template <int DT>
 struct Raw { typedef uint4 type; };
@@ -90,10 +88,10 @@ struct Raw<BRL_I8> { typedef uint2 type; };
 template <class S>
 struct KeyLoads {
     typename Raw<S::DT>::type raw[2][S::KS][S::KL];
-    __device__ __forceinline__ void request(const char* pool, const Block& b, int lane) {
+    __device__ __forceinline__ void request(const char* pool, int lo, int hi, int lane) {
         const int c = lane & 15, g = lane >> 4;
-        const long long row = (c >> 3) ? b.hi : b.lo;
-        const char* p = pool + (row < 0 ? 0 : row) * (long long)S::RB + (((c >> 2) & 1) * 8 + (c & 3)) * S::RB + 8 * g * S::SZ;
+        const char *pl = pool + (size_t)(lo < 0 ? 0 : lo) * S::RB, *ph = pool + (size_t)(hi < 0 ? 0 : hi) * S::RB;
+        const char* p = ((c >> 3) ? ph : pl) + (unsigned)((((c >> 2) & 1) * 8 + (c & 3)) * S::RB + 8 * g * S::SZ);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -137,25 +135,25 @@ struct KeyLoads {
 template <class S>
 struct ValueLoads {
     uint4 raw[S::NV];
-    __device__ __forceinline__ void request(const char* pool, const Block& b, int lane) {
-        const char* lo = pool + (b.lo < 0 ? 0 : b.lo) * (long long)S::RB;
-        const char* hi = pool + (b.hi < 0 ? 0 : b.hi) * (long long)S::RB - 16 * S::RB;
+    __device__ __forceinline__ void request(const char* pool, int lo_row, int hi_row, int lane) {
+        const char* lo = pool + (size_t)(lo_row < 0 ? 0 : lo_row) * S::RB;
+        const char* hi = pool + (size_t)(hi_row < 0 ? 0 : hi_row) * S::RB;
+        constexpr int HALF = 16 * S::CPR;                              // chunks of 16 rows
 #pragma unroll
         for (int i = 0; i < S::NV; ++i) {
             const int idx = i * 64 + lane;
             if (S::NV * 64 > 32 * S::CPR && idx >= 32 * S::CPR) continue;
-            raw[i] = *reinterpret_cast<const uint4*>((idx >= 16 * S::CPR ? hi : lo) + idx * 16);
+            if ((i + 1) * 64 <= HALF) raw[i] = reinterpret_cast<const uint4*>(lo + i * 1024)[(unsigned)lane];
+            else if (i * 64 >= HALF) raw[i] = reinterpret_cast<const uint4*>(hi + (i * 64 - HALF) * 16)[(unsigned)lane];
+            else raw[i] = idx >= HALF ? reinterpret_cast<const uint4*>(hi)[(unsigned)(idx - HALF)] : reinterpret_cast<const uint4*>(lo)[(unsigned)idx];
         }
     }
-    // there: keys first .. last - 1 of the block hold numbers (the others are stored as zeros)
-    template <bool MASK>
-    __device__ __forceinline__ void store(char* lds, int lane, uint32_t there) const {
+    __device__ __forceinline__ void store(char* lds, int lane) const {
 #pragma unroll
         for (int i = 0; i < S::NV; ++i) {
             const int idx = i * 64 + lane, key = idx / S::CPR, c = idx % S::CPR;
             if (S::NV * 64 > 32 * S::CPR && idx >= 32 * S::CPR) continue;
-            uint4 r = raw[i];
-            if (MASK && !(there >> key & 1u)) r = make_uint4(0, 0, 0, 0);
+            const uint4 r = raw[i];
             if constexpr (S::DT == BRL_F16) {
                 *reinterpret_cast<uint4*>(lds + lds_chunk<S>(key, c)) = r;
             } else if constexpr (S::DT == BRL_F32) {
@@ -177,88 +175,98 @@ struct ValueLoads {
         }
     }
 };
-
-// Transposed value fragment: of components 16 d + (lane & 15) the keys 8 g .. 8 g + 7.  A transposing read gives each lane
-// of 16 one column of 4 rows x 16 halfs whose row i the lanes 4 i .. 4 i + 3 address.
+// rows of a stored block that hold no numbers: zeros (bit `key` of there is clear)
 template <class S>
-__device__ __forceinline__ v8h value_fragment(const char* lds, int d, int lane) {
-    const int c = lane & 15, g = lane >> 4;
-    uint2 r[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int key = 8 * g + 4 * u + (c >> 2);
-        const char* p = lds + lds_chunk<S>(key, 2 * d + ((c & 3) >> 1)) + (c & 1) * 8;
-        typedef __attribute__((address_space(3))) v4fp* lds_ptr;
-        const v4fp x = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_ptr)(p));
-        r[u] = __builtin_bit_cast(uint2, x);
-    }
-    return __builtin_bit_cast(v8h, make_uint4(r[0].x, r[0].y, r[1].x, r[1].y));
+__device__ __forceinline__ void clear_rows(char* lds, int lane, uint32_t there) {
+#pragma unroll 1
+    for (int i = lane; i < S::PL * 32 * S::NCH; i += 64)
+        if (!(there >> (i / S::NCH % 32) & 1u)) reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
 }
 
-// the 16 query rows of a tile, rotated, scaled and split: lane 16 g + c holds components 32 s + 8 g .. of row c
+// Transposed value fragment: of components 16 d + (lane & 15) the keys 8 g .. 8 g + 7.  A transposing read gives each lane
+// of 16 one column of 4 rows x 16 halfs whose row i the lanes 4 i .. 4 i + 3 address.  (Keys four apart have their chunks
+// permuted alike, so the second read is the first one's address and a constant.)
 template <class S>
-struct QueryTile {
-    v8h hi[S::KS], lo[S::KS];
-    __device__ __forceinline__ void load(const CachedAttention& a, const StateTokens& st, int h, int group, int r, int rows, int lane) {
-        constexpr int DH = S::DH, half = DH / 2;
-        const int g = lane >> 4;
-        const float scale = (float)(1.0 / sqrt((double)DH)) * LOG2E;
-        const bool live = r < rows;
-        const int i = live ? r / group : 0, head = h * group + (live ? r % group : 0);
-        const int row = st.row0 + i, pos = rope_position(a.t, row, st.base + i);
-        const float* x = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * DH) + head * DH;
-        const float *ct = a.t.cos_t + (size_t)pos * half, *sn = a.t.sin_t + (size_t)pos * half;
+struct ValueReads {
+    const char* base;
+    int x;
+    __device__ __forceinline__ ValueReads(const char* lds, int lane) {
+        const int c = lane & 15, key = 8 * (lane >> 4) + (c >> 2);
+        const int at = lds_chunk<S>(key, (c & 3) >> 1);
+        base = lds + key * S::LS + (c & 1) * 8;
+        x = at - key * S::LS;
+    }
+    __device__ __forceinline__ v8h fragment(int d, int plane) const {
+        uint2 r[2];
+        const char* p = base + (x ^ (d << 5));
 #pragma unroll
-        for (int s = 0; s < S::KS; ++s) {
-            float y[8];
-            const int d0 = 32 * s + 8 * g;
-            if constexpr (DH % 16 == 0) {                              // eight components lie in one half
-                const bool in = live && d0 < DH;
-                const int d = d0 < DH ? d0 : 0, f = d < half ? d : d - half, partner = d < half ? d + half : d - half;
-                float u[8], v[8], c[8], w[8];
-#pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    *reinterpret_cast<float4*>(u + e) = *reinterpret_cast<const float4*>(x + d + e);
-                    *reinterpret_cast<float4*>(v + e) = *reinterpret_cast<const float4*>(x + partner + e);
-                    *reinterpret_cast<float4*>(c + e) = *reinterpret_cast<const float4*>(ct + f + e);
-                    *reinterpret_cast<float4*>(w + e) = *reinterpret_cast<const float4*>(sn + f + e);
-                }
-                const float sign = d < half ? -1.f : 1.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = in ? (u[e] * c[e] + sign * (v[e] * w[e])) * scale : 0.f;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool in = live && d0 + e < DH;
-                    const int d = d0 + e < DH ? d0 + e : 0, f = d < half ? d : d - half, partner = d < half ? d + half : d - half;
-                    const float p = x[partner] * sn[f];
-                    y[e] = in ? (x[d] * ct[f] + (d < half ? -p : p)) * scale : 0.f;
-                }
-            }
-            uint32_t a4[4], b4[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) split_pair(y[2 * e], y[2 * e + 1], a4[e], b4[e]);
-            hi[s] = __builtin_bit_cast(v8h, make_uint4(a4[0], a4[1], a4[2], a4[3]));
-            lo[s] = __builtin_bit_cast(v8h, make_uint4(b4[0], b4[1], b4[2], b4[3]));
+        for (int u = 0; u < 2; ++u) {
+            typedef __attribute__((address_space(3))) v4fp* lds_ptr;
+            const v4fp v = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_ptr)(p + plane * S::PLANE + u * 4 * S::LS));
+            r[u] = __builtin_bit_cast(uint2, v);
         }
+        return __builtin_bit_cast(v8h, make_uint4(r[0].x, r[0].y, r[1].x, r[1].y));
     }
 };
 
-// which of the keys 8 g + e of a block row (token i) sees, for blocks that not every row sees whole
+// Query rows, rotated, scaled and split, as operand fragments in LDS: [row tile][step][hi, lo][64 lanes] of 16 bytes; lane
+// 16 g + c of a fragment holds components 32 s + 8 g .. of row c.  A job is one lane of one (row tile, step).
+template <class S>
+struct QueryJob {
+    float x[8], y[8], c[8], w[8];      // components, their partners, cosines, sines
+    __device__ __forceinline__ void request(const CachedAttention& a, const StateTokens& st, int h, int group, int rows, int job) {
+        constexpr int DH = S::DH, half = DH / 2;
+        const int lane = job & 63, s = (job >> 6) % S::KS, r0 = (job >> 6) / S::KS * 16 + (lane & 15), r = r0 < rows ? r0 : rows - 1;
+        const int i = r / group, row = st.row0 + i, pos = rope_position(a.t, row, st.base + i), d0 = 32 * s + 8 * (lane >> 4);
+        const float* q = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * DH) + (h * group + r % group) * DH;
+        const float *ct = a.t.cos_t + (size_t)pos * half, *sn = a.t.sin_t + (size_t)pos * half;
+        if constexpr (DH % 16 == 0) {                                  // eight components lie in one half
+            const int d = d0 < DH ? d0 : 0, f = d < half ? d : d - half, partner = d < half ? d + half : d - half;
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                *reinterpret_cast<float4*>(x + e) = *reinterpret_cast<const float4*>(q + d + e);
+                *reinterpret_cast<float4*>(y + e) = *reinterpret_cast<const float4*>(q + partner + e);
+                *reinterpret_cast<float4*>(c + e) = *reinterpret_cast<const float4*>(ct + f + e);
+                *reinterpret_cast<float4*>(w + e) = *reinterpret_cast<const float4*>(sn + f + e);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int d = d0 + e < DH ? d0 + e : 0, f = d < half ? d : d - half, partner = d < half ? d + half : d - half;
+                x[e] = q[d]; y[e] = q[partner]; c[e] = ct[f]; w[e] = sn[f];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(uint4* lds, int rows, int job) const {
+        constexpr int DH = S::DH, half = DH / 2;
+        const float scale = (float)(1.0 / sqrt((double)DH)) * LOG2E;
+        const int lane = job & 63, s = (job >> 6) % S::KS, rt = (job >> 6) / S::KS, d0 = 32 * s + 8 * (lane >> 4);
+        const bool live = rt * 16 + (lane & 15) < rows;
+        uint32_t hi[4], lo[4];
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p = y[e] * w[e];
+            z[e] = live && d0 + e < DH ? (x[e] * c[e] + (d0 + e < half ? -p : p)) * scale : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) split_pair(z[2 * e], z[2 * e + 1], hi[e], lo[e]);
+        lds[((rt * S::KS + s) * 2) * 64 + lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        lds[((rt * S::KS + s) * 2 + 1) * 64 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+};
+
+// which of the slots slot0 .. slot0 + 7 token i sees, for blocks that not every row sees whole
 __device__ __forceinline__ uint32_t visible_bits(const CachedAttention& a, const StateTokens& st, int i, int slot0) {
     if (!a.tree) {
-        const int n = st.base + i + 1 - slot0;                         // keys from slot0 on that are seen
+        const int n = st.base + i + 1 - slot0;                         // from slot0 on
         return n >= 8 ? 0xffu : n <= 0 ? 0u : (1u << n) - 1u;
     }
-    uint32_t bits = 0;
+    const int j = slot0 - st.base, w = j >> 5;                         // bits j .. j + 7, set in front of the mask, clear behind it
     const uint32_t* mask = a.tree + (size_t)(st.row0 + i) * a.mask_words;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int j = slot0 + e - st.base;
-        const bool see = j < 0 || ((j >> 5) < a.mask_words && (mask[j >> 5] >> (j & 31) & 1u));
-        bits |= see ? 1u << e : 0u;
-    }
-    return bits;
+    const uint32_t lo = w < 0 ? 0xffffffffu : w < a.mask_words ? mask[w] : 0u;
+    const uint32_t hi = w + 1 < 0 ? 0xffffffffu : w + 1 < a.mask_words ? mask[w + 1] : 0u;
+    return (uint32_t)((((uint64_t)hi << 32) | lo) >> (j & 31)) & 0xffu;
 }
 
 // ---- running softmax and sum of one tile of 16 rows ----
@@ -300,7 +308,7 @@ struct RowState {
 
 // One wavefront's pass over a block: scores of RT row tiles against the block's 32 keys
 template <class S, int RT>
-__device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const QueryTile<S> (&q)[RT], int lane, float (&s)[RT][8]) {
+__device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const uint4* q, int lane, float (&s)[RT][8]) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         v4f acc[RT];
@@ -312,9 +320,11 @@ __device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const QueryTi
             k.fragment(t, st, lane, f);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                if constexpr (S::PL == 2) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1], q[r].hi[st], acc[r], 0, 0, 0);
-                acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0], q[r].lo[st], acc[r], 0, 0, 0);
-                acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0], q[r].hi[st], acc[r], 0, 0, 0);
+                const v8h qh = __builtin_bit_cast(v8h, q[((r * S::KS + st) * 2) * 64 + lane]);
+                const v8h ql = __builtin_bit_cast(v8h, q[((r * S::KS + st) * 2 + 1) * 64 + lane]);
+                if constexpr (S::PL == 2) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1], qh, acc[r], 0, 0, 0);
+                acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0], ql, acc[r], 0, 0, 0);
+                acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0], qh, acc[r], 0, 0, 0);
             }
         }
 #pragma unroll
@@ -335,11 +345,12 @@ __device__ __forceinline__ void block_values(const char* lds, const float (&p)[R
         ph[r] = __builtin_bit_cast(v8h, make_uint4(h[0], h[1], h[2], h[3]));
         pl[r] = __builtin_bit_cast(v8h, make_uint4(l[0], l[1], l[2], l[3]));
     }
+    const ValueReads<S> v(lds, lane);
 #pragma unroll
     for (int d = 0; d < S::DTL; ++d) {
         v8h f[S::PL];
 #pragma unroll
-        for (int x = 0; x < S::PL; ++x) f[x] = value_fragment<S>(lds + x * S::PLANE, d, lane);
+        for (int x = 0; x < S::PL; ++x) f[x] = v.fragment(d, x);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             if constexpr (S::PL == 2) st[r].o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1], ph[r], st[r].o[d], 0, 0, 0);
@@ -351,10 +362,12 @@ __device__ __forceinline__ void block_values(const char* lds, const float (&p)[R
 
 struct Plan {
     int group, rows_max;      // query heads per k/v head; rows of a state at most
-    int row_blocks, splits;   // workgroups per (state, k/v head): blocks of rows, parts of the keys
     int rows_pad;             // rows reserved per (state, k/v head) in the scratch space
-    float* part_o;            // [B][n_kv][rows_pad][splits][dh], relative to part_ml's reference
-    float2* part_ml;          // [B][n_kv][rows_pad][splits]: reference and sum
+    int groups;               // workgroups that share all blocks evenly, 0: one workgroup per (state, k/v head)
+    int least;                // blocks a workgroup takes at least
+    float* part_o;            // [2 groups][rows_pad][dh]: sums relative to part_ml's reference
+    float2* part_ml;          // [2 groups][rows_pad]: reference and sum of probabilities
+    float* lse;               // [B][n_kv][rows_pad] or nullptr: log2 of a row's sum, +inf where it sees nothing
     float* scores;            // [B][n_kv][rows_pad][ld_scores] or nullptr
     size_t ld_scores;
 };
@@ -363,257 +376,343 @@ __device__ __forceinline__ float* out_row(const CachedAttention& a, const StateT
     return a.out + ((size_t)(st.row0 + r / group) * a.n_heads + h * group + r % group) * a.c.dh;
 }
 
-// ---- few rows: every wavefront of a workgroup walks its own blocks of the workgroup's part of the keys ----
-// Nothing is shared between wavefronts before the end: keys go from memory into operand registers, values through a region of LDS of the
-// wavefront's own, where the transposing reads turn them.  The next block's keys are requested as soon as the scores have been
-// taken, its values as soon as this block's have been stored, so that loads are in flight all the time.
+// ---- sharing the work ----
+// The blocks of 32 slots of all (state, k/v head) pairs, in that order, are one list; workgroup w takes the entries
+// w share .. (w + 1) share - 1.  States of different length so cost every workgroup the same.
+__device__ __forceinline__ int state_blocks(const CachedAttention& a, int b) {
+    const StateTokens st = state_tokens(a.t, a.c, b);
+    return st.n ? (st.len + 31) >> 5 : 0;
+}
+// Per wavefront: blocks of the states in front of this lane's stretch of states, and of all.
+struct Prefix {
+    int stretch;              // states per lane
+    int before, total;
+};
+__device__ __forceinline__ Prefix prefix_blocks(const CachedAttention& a, int lane) {
+    Prefix p;
+    p.stretch = (a.t.B + 63) / 64;
+    int mine = 0;
+    for (int b = lane * p.stretch; b < (lane + 1) * p.stretch && b < a.t.B; ++b) mine += state_blocks(a, b);
+    int x = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d, 64);
+        if (lane >= d) x += y;
+    }
+    p.before = x - mine;
+    p.total = lane_value(x, 63);
+    return p;
+}
+__device__ __forceinline__ int share_of(const Plan& p, long long entries) {
+    const long long s = (entries + p.groups - 1) / p.groups;
+    return s < p.least ? p.least : (int)s;
+}
+
+// ---- few rows: every wavefront of a workgroup walks its own blocks ----
+// Nothing is shared between wavefronts but the query rows: keys go from memory into operand registers, values through a region of
+// LDS of the wavefront's own, where the transposing reads turn them.  The next block's keys are requested as soon as the scores
+// have been taken, its values as soon as this block's have been stored, so that loads are in flight all the time.
 template <int DT, int DH, int RT>
 __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a, Plan p) {
     typedef Shape<DT, DH> S;
     extern __shared__ __attribute__((aligned(16))) char lds_all[];
+    __shared__ uint4 s_q[RT * S::KS * 2 * 64];
     __shared__ float2 s_ml[8][RT * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const int split = blockIdx.x % p.splits, h = blockIdx.x / p.splits % a.c.n_kv, b = blockIdx.x / p.splits / a.c.n_kv;
-    const StateTokens st = state_tokens(a.t, a.c, b);
-    const int rows = st.n * p.group;
-    if (rows == 0) return;
     const int c = lane & 15, g = lane >> 4;
     char* lds = lds_all + wave * S::LDS;
-    const int seen = st.len;                                           // (the last token sees them all, or bits of the mask)
-    const int blocks = (seen + 31) >> 5, per = (blocks + p.splits - 1) / p.splits;
-    const int first = split * per, last = first + per < blocks ? first + per : blocks;
 
-    QueryTile<S> q[RT];
-    RowState<S> row[RT];
-    float unit = 0x1p126f;                                             // int8: power of two that the sums are multiplied by
-    // the first token of each row tile decides up to where all of its rows see everything
-    int token[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        row[r].clear();
-        token[r] = (r * 16 + c < rows ? r * 16 + c : rows - 1) / p.group;
-    }
-    const int all_see = st.base + (a.tree ? 0 : 1);                    // slots below are seen by every row (causal: by token 0)
-
-    long long page_lo = -1, page_hi = -1;                              // of the lane-th block ahead
-    auto pages = [&](int t0) {
-        const int slot = (t0 + lane * waves) * 32;
-        page_lo = slot < seen ? kv_row_index(a.c, b, h, slot) : -1;
-        page_hi = slot + 16 < seen ? kv_row_index(a.c, b, h, slot + 16) : -1;
-    };
-    auto block_at = [&](int i) {
-        Block x;
-        x.lo = lane_value(page_lo, i);
-        x.hi = lane_value(page_hi, i);
-        return x;
-    };
-    KeyLoads<S> keys;
-    ValueLoads<S> values;
-    Block cur;
-    float4 ks[2], vs[2];                                               // int8: scales of keys 8 g .. 8 g + 7
-    auto key_scales = [&](const Block& x) {
-        const long long r = (g >> 1) ? x.hi : x.lo;
-        const float* f = a.c.ks + (r < 0 ? 0 : r) + (g & 1) * 8;
-        ks[0] = reinterpret_cast<const float4*>(f)[0];
-        ks[1] = reinterpret_cast<const float4*>(f)[1];
-    };
-    auto value_scales = [&](const Block& x) {
-        const long long r = (g >> 1) ? x.hi : x.lo;
-        const float* f = a.c.vs + (r < 0 ? 0 : r) + (g & 1) * 8;
-        vs[0] = reinterpret_cast<const float4*>(f)[0];
-        vs[1] = reinterpret_cast<const float4*>(f)[1];
-    };
-    int t = first + wave, ahead = 0;
-    if (t < last) {
-        pages(t);
-        cur = block_at(0);
-        keys.request(a.c.k, cur, lane);
-        if constexpr (DT == BRL_I8) key_scales(cur);
-        values.request(a.c.v, cur, lane);
-        if constexpr (DT == BRL_I8) value_scales(cur);
-    }
-#pragma unroll
-    for (int r = 0; r < RT; ++r) q[r].load(a, st, h, p.group, r * 16 + c, rows, lane);
-    for (; t < last; t += waves) {
-        const int slot0 = t * 32;
-        float s[RT][8];
-        block_scores<S, RT>(keys, q, lane, s);
-        if constexpr (DT == BRL_I8) {
-            const float f[8] = {ks[0].x, ks[0].y, ks[0].z, ks[0].w, ks[1].x, ks[1].y, ks[1].z, ks[1].w};
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[r][e] *= f[e];
+    // this workgroup's entries: left of them, the state and head they begin in, the block in it
+    int b, h, block;
+    long long left;
+    if (p.groups == 0) {
+        h = blockIdx.x % a.c.n_kv; b = blockIdx.x / a.c.n_kv; block = 0;
+        left = 1ll << 40;
+    } else {
+        const Prefix pre = prefix_blocks(a, lane);
+        const long long entries = (long long)pre.total * a.c.n_kv;
+        const int share = share_of(p, entries);
+        long long at = (long long)blockIdx.x * share;
+        left = entries - at < share ? entries - at : share;
+        if (left <= 0) return;
+        const unsigned long long in = __ballot((long long)pre.before * a.c.n_kv <= at);
+        const int l = 63 - __builtin_clzll(in);                         // the last stretch that begins at or before the entry
+        at -= (long long)lane_value(pre.before, l) * a.c.n_kv;
+        b = l * pre.stretch;
+        int n = state_blocks(a, b);
+        while (at >= (long long)n * a.c.n_kv) {
+            at -= (long long)n * a.c.n_kv;
+            n = state_blocks(a, ++b);
         }
-        // the next block's keys
-        Block next = cur;
-        const bool more = t + waves < last;
-        if (more) {
+        h = (int)(at / n);
+        block = (int)(at % n);
+    }
+    bool before = true;                                                // nothing but this segment's beginning lies in front
+    for (;;) {
+        const StateTokens st = state_tokens(a.t, a.c, b);
+        const int rows = st.n * p.group, seen = st.len;                // (the last token sees them all, or bits of the mask)
+        const int blocks = rows ? (seen + 31) >> 5 : 0;
+        const int first = block, last = left < blocks - block ? block + (int)left : blocks;
+        if (rows) {
+        const bool all = first == 0 && last == blocks;
+        QueryJob<S> q;
+        constexpr int JOBS = RT * S::KS * 64;
+        static_assert(JOBS <= 512, "two jobs a thread at most");
+        if (threadIdx.x < JOBS) q.request(a, st, h, p.group, rows, threadIdx.x);
+        RowState<S> row[RT];
+        float unit = 0x1p126f;                                         // int8: power of two that the sums are multiplied by
+        int token[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            row[r].clear();
+            token[r] = (r * 16 + c < rows ? r * 16 + c : rows - 1) / p.group;
+        }
+        const int all_see = st.base + (a.tree ? 0 : 1);                // slots below are seen by every row (causal: by token 0)
+
+        int page_lo = -1, page_hi = -1;                                // rows of the lane-th block ahead
+        auto pages = [&](int t0) {
+            const int slot = (t0 + lane * waves) * 32;
+            page_lo = slot < seen ? kv_row_index(a.c, b, h, slot) : -1;
+            page_hi = slot + 16 < seen ? kv_row_index(a.c, b, h, slot + 16) : -1;
+        };
+        KeyLoads<S> keys;
+        ValueLoads<S> values;
+        int lo = -1, hi = -1;                                          // where the current block lies
+        float4 ks[2], vs[2];                                           // int8: scales of keys 8 g .. 8 g + 7
+        auto scales = [&](const float* pool, int x_lo, int x_hi, float4 (&f)[2]) {
+            const int r = (g >> 1) ? x_hi : x_lo;
+            const float* y = pool + (r < 0 ? 0 : r) + (g & 1) * 8;
+            f[0] = reinterpret_cast<const float4*>(y)[0];
+            f[1] = reinterpret_cast<const float4*>(y)[1];
+        };
+        int t = first + wave, ahead = 0;
+        if (t < last) {
+            pages(t);
+            lo = lane_value(page_lo, 0);
+            hi = lane_value(page_hi, 0);
+            keys.request(a.c.k, lo, hi, lane);
+            if constexpr (DT == BRL_I8) scales(a.c.ks, lo, hi, ks);
+            values.request(a.c.v, lo, hi, lane);
+            if constexpr (DT == BRL_I8) scales(a.c.vs, lo, hi, vs);
+        }
+        if (threadIdx.x < JOBS) q.store(s_q, rows, threadIdx.x);
+        if constexpr (JOBS > 256) {
+            const int job = blockDim.x + threadIdx.x;
+            if (job < JOBS) {
+                q.request(a, st, h, p.group, rows, job);
+                q.store(s_q, rows, job);
+            }
+        }
+        __syncthreads();
+        for (; t < last; t += waves) {
+            const int slot0 = t * 32;
+            int at = lane;                                             // (opaque: or the compiler keeps all of LDS in registers)
+            asm volatile("" : "+v"(at));
+            float s[RT][8];
+            block_scores<S, RT>(keys, s_q, at, s);
+            if constexpr (DT == BRL_I8) {
+                const float f[8] = {ks[0].x, ks[0].y, ks[0].z, ks[0].w, ks[1].x, ks[1].y, ks[1].z, ks[1].w};
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[r][e] *= f[e];
+            }
+            __builtin_amdgcn_sched_barrier(0);                         // (the old keys' registers are free from here on)
+            // Behind the last block, rows 0 of the pool are requested and never used: a request that might not be made would
+            // have every wait in the loop wait for all of them.
             if (++ahead == 64) {
                 ahead = 0;
                 pages(t + waves);
             }
-            next = block_at(ahead);
-            keys.request(a.c.k, next, lane);
-            if constexpr (DT == BRL_I8) key_scales(next);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        const bool whole = slot0 + 32 <= all_see && cur.lo >= 0 && cur.hi >= 0;
-        float vf[8];
-        if constexpr (DT == BRL_I8) {
-            const float f[8] = {vs[0].x, vs[0].y, vs[0].z, vs[0].w, vs[1].x, vs[1].y, vs[1].z, vs[1].w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) vf[e] = f[e];
-        }
-        if (whole) {
-            values.template store<false>(lds, lane, 0);
-        } else {
-            const int n = seen - slot0;
-            uint32_t there = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
-            if (cur.lo < 0) there &= 0xffff0000u;
-            if (cur.hi < 0) there &= 0x0000ffffu;
-            values.template store<true>(lds, lane, there);
-            const uint32_t mine = there >> (8 * g) & 0xffu;
+            const bool more = t + waves < last;
+            const int next_lo = more ? lane_value(page_lo, ahead) : -1, next_hi = more ? lane_value(page_hi, ahead) : -1;
+            keys.request(a.c.k, next_lo, next_hi, lane);
+            if constexpr (DT == BRL_I8) scales(a.c.ks, next_lo, next_hi, ks);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool whole = slot0 + 32 <= all_see && lo >= 0 && hi >= 0;
+            float vf[8];
             if constexpr (DT == BRL_I8) {
+                const float f[8] = {vs[0].x, vs[0].y, vs[0].z, vs[0].w, vs[1].x, vs[1].y, vs[1].z, vs[1].w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) vf[e] = mine >> e & 1u ? vf[e] : 0.f;
+                for (int e = 0; e < 8; ++e) vf[e] = f[e];
             }
+            values.store(lds, at);
+            if (!whole) {
+                const int n = seen - slot0;
+                uint32_t there = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+                if (lo < 0) there &= 0xffff0000u;
+                if (hi < 0) there &= 0x0000ffffu;
+                if (there != 0xffffffffu) clear_rows<S>(lds, lane, there);
+                const uint32_t mine = there >> (8 * g) & 0xffu;
+                if constexpr (DT == BRL_I8) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const uint32_t bits = mine & visible_bits(a, st, token[r], slot0 + 8 * g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[r][e] = bits >> e & 1u ? s[r][e] : -INFINITY;
-            }
-        }
-        if (more) {
-            values.request(a.c.v, next, lane);
-            if constexpr (DT == BRL_I8) value_scales(next);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        if (p.scores) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-                if (r * 16 + c < rows) {
-                    float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_pad + r * 16 + c) * p.ld_scores + slot0 + 8 * g;
-                    reinterpret_cast<float4*>(f)[0] = make_float4(s[r][0], s[r][1], s[r][2], s[r][3]);
-                    reinterpret_cast<float4*>(f)[1] = make_float4(s[r][4], s[r][5], s[r][6], s[r][7]);
+                    for (int e = 0; e < 8; ++e) vf[e] = mine >> e & 1u ? vf[e] : 0.f;
                 }
-        }
 #pragma unroll
-        for (int r = 0; r < RT; ++r) row[r].probabilities(s[r]);
-        if constexpr (DT == BRL_I8) {
-            // scales relative to the largest so far, a power of two that only falls: fp16 holds the products
-            float top = vf[0];
+                for (int r = 0; r < RT; ++r) {
+                    const uint32_t bits = mine & visible_bits(a, st, token[r], slot0 + 8 * g);
 #pragma unroll
-            for (int e = 1; e < 8; ++e) top = fmaxf(top, vf[e]);
-            if (__any(top * unit > 1.f)) {
-                const float now = __builtin_amdgcn_exp2f(-ceilf(__builtin_amdgcn_logf(wave_max(top))) - 1.f);
-                const float f = now / unit;
+                    for (int e = 0; e < 8; ++e) s[r][e] = bits >> e & 1u ? s[r][e] : -INFINITY;
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            values.request(a.c.v, next_lo, next_hi, lane);
+            if constexpr (DT == BRL_I8) scales(a.c.vs, next_lo, next_hi, vs);
+            __builtin_amdgcn_sched_barrier(0);
+            if (p.scores) {
 #pragma unroll
-                for (int r = 0; r < RT; ++r) row[r].scale(f);
-                unit = now;
+                for (int r = 0; r < RT; ++r)
+                    if (r * 16 + c < rows) {
+                        float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_pad + r * 16 + c) * p.ld_scores + slot0 + 8 * g;
+                        reinterpret_cast<float4*>(f)[0] = make_float4(s[r][0], s[r][1], s[r][2], s[r][3]);
+                        reinterpret_cast<float4*>(f)[1] = make_float4(s[r][4], s[r][5], s[r][6], s[r][7]);
+                    }
             }
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
+            for (int r = 0; r < RT; ++r) row[r].probabilities(s[r]);
+            if constexpr (DT == BRL_I8) {
+                // scales relative to the largest so far, a power of two that only falls: fp16 holds the products
+                float top = vf[0];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s[r][e] *= vf[e] * unit;
-        }
-        __builtin_amdgcn_wave_barrier();
-        block_values<S, RT>(lds, s, row, lane);
-        __builtin_amdgcn_wave_barrier();
-        cur = next;
-    }
-    // the wavefronts' parts meet: sums to the largest reference, then O over LDS, a row tile at a time
+                for (int e = 1; e < 8; ++e) top = fmaxf(top, vf[e]);
+                if (__any(top * unit > 1.f)) {
+                    const float now = __builtin_amdgcn_exp2f(-ceilf(__builtin_amdgcn_logf(wave_max(top))) - 1.f);
+                    const float f = now / unit;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        row[r].l += __shfl_xor(row[r].l, 16, 64);
-        row[r].l += __shfl_xor(row[r].l, 32, 64);
-        if (g == 0) s_ml[wave][r * 16 + c] = make_float2(row[r].l > 0.f ? row[r].ref : -INFINITY, row[r].l);
-    }
-    __syncthreads();
+                    for (int r = 0; r < RT; ++r) row[r].scale(f);
+                    unit = now;
+                }
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        float top = -INFINITY;
-        for (int w = 0; w < waves; ++w) top = fmaxf(top, s_ml[w][r * 16 + c].x);
-        float f = row[r].l > 0.f ? __builtin_amdgcn_exp2f(row[r].ref - top) : 0.f;
-        if constexpr (DT == BRL_I8) f /= unit;
-        float* o = reinterpret_cast<float*>(lds);                      // [16 rows][ROW]
+                for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int d = 0; d < S::DTL; ++d) *reinterpret_cast<v4f*>(o + c * S::ROW + 16 * d + 4 * g) = row[r].o[d] * f;
-        __syncthreads();
-        for (int i = threadIdx.x; i < 16 * S::ROW / 4; i += blockDim.x) {
-            const int x = i / (S::ROW / 4), d = i % (S::ROW / 4) * 4, rr = r * 16 + x;
-            if (rr >= rows || d >= DH) continue;
-            float ref = -INFINITY, l = 0.f;
-            for (int w = 0; w < waves; ++w) ref = fmaxf(ref, s_ml[w][rr].x);
-            v4f sum = {0.f, 0.f, 0.f, 0.f};
-            for (int w = 0; w < waves; ++w) {
-                const float2 ml = s_ml[w][rr];
-                if (ml.y > 0.f) l += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
-                sum += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds_all + w * S::LDS) + x * S::ROW + d);
+                    for (int e = 0; e < 8; ++e) s[r][e] *= vf[e] * unit;
             }
-            const size_t at = (((size_t)b * a.c.n_kv + h) * p.rows_pad + rr) * p.splits + split;
-            if (p.part_ml && d == 0) p.part_ml[at] = make_float2(ref, l);
-            if (p.splits > 1) *reinterpret_cast<v4f*>(p.part_o + at * DH + d) = sum;
-            else *reinterpret_cast<v4f*>(out_row(a, st, h, p.group, rr) + d) = sum * (l > 0.f ? 1.f / l : 0.f);
+            __builtin_amdgcn_wave_barrier();
+            block_values<S, RT>(lds, s, row, at);
+            __builtin_amdgcn_wave_barrier();
+            lo = next_lo;
+            hi = next_hi;
+        }
+        // the wavefronts' parts meet: sums to the largest reference, then O over LDS, a row tile at a time
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            row[r].l += __shfl_xor(row[r].l, 16, 64);
+            row[r].l += __shfl_xor(row[r].l, 32, 64);
+            if (g == 0) s_ml[wave][r * 16 + c] = make_float2(row[r].l > 0.f ? row[r].ref : -INFINITY, row[r].l);
         }
         __syncthreads();
+        const size_t slot = 2 * (size_t)blockIdx.x + (before ? 0 : 1);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float top = -INFINITY;
+            for (int w = 0; w < waves; ++w) top = fmaxf(top, s_ml[w][r * 16 + c].x);
+            float f = row[r].l > 0.f ? __builtin_amdgcn_exp2f(row[r].ref - top) : 0.f;
+            if constexpr (DT == BRL_I8) f /= unit;
+            float* o = reinterpret_cast<float*>(lds);                  // [16 rows][ROW]
+#pragma unroll
+            for (int d = 0; d < S::DTL; ++d) *reinterpret_cast<v4f*>(o + c * S::ROW + 16 * d + 4 * g) = row[r].o[d] * f;
+            __syncthreads();
+            for (int i = threadIdx.x; i < 16 * S::ROW / 4; i += blockDim.x) {
+                const int x = i / (S::ROW / 4), d = i % (S::ROW / 4) * 4, rr = r * 16 + x;
+                if (rr >= rows || d >= DH) continue;
+                float ref = -INFINITY, l = 0.f;
+                for (int w = 0; w < waves; ++w) ref = fmaxf(ref, s_ml[w][rr].x);
+                v4f sum = {0.f, 0.f, 0.f, 0.f};
+                for (int w = 0; w < waves; ++w) {
+                    const float2 ml = s_ml[w][rr];
+                    if (ml.y > 0.f) l += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
+                    sum += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds_all + w * S::LDS) + x * S::ROW + d);
+                }
+                if (all) {
+                    *reinterpret_cast<v4f*>(out_row(a, st, h, p.group, rr) + d) = sum * (l > 0.f ? 1.f / l : 0.f);
+                    if (p.lse && d == 0)
+                        p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + rr] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
+                } else {
+                    *reinterpret_cast<v4f*>(p.part_o + (slot * p.rows_pad + rr) * DH + d) = sum;
+                    if (d == 0) p.part_ml[slot * p.rows_pad + rr] = make_float2(ref, l);
+                }
+            }
+            __syncthreads();
+        }
+        }
+        if (p.groups == 0) return;
+        left -= last - first;
+        if (left <= 0) return;
+        before = false;
+        block = 0;
+        if (++h == a.c.n_kv || blocks == 0) {
+            h = 0;
+            ++b;
+        }
     }
 }
 
-// ---- the parts of the keys joined: a wavefront per row ----
+// ---- the parts of a (state, k/v head) that several workgroups took, joined: a workgroup per row ----
+template <int DH>
 __global__ __launch_bounds__(256) void cached_join_kernel(CachedAttention a, Plan p) {
-    const int lane = threadIdx.x & 63;
-    const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int r = (int)(unit % p.rows_max), h = (int)(unit / p.rows_max % a.c.n_kv);
-    const long long b = unit / p.rows_max / a.c.n_kv;
-    if (b >= a.t.B) return;
-    const StateTokens st = state_tokens(a.t, a.c, (int)b);
+    constexpr int LANES = DH == 100 ? 32 : DH / 4, PARTS = 256 / LANES;
+    __shared__ __attribute__((aligned(16))) float s_o[PARTS][DH];
+    const int r = blockIdx.x % p.rows_max, h = blockIdx.x / p.rows_max % a.c.n_kv, b = blockIdx.x / p.rows_max / a.c.n_kv;
+    const StateTokens st = state_tokens(a.t, a.c, b);
     if (r >= st.n * p.group) return;
-    const size_t at = (((size_t)b * a.c.n_kv + h) * p.rows_pad + r) * p.splits;
-    float ref = -INFINITY;
-    for (int s = lane; s < p.splits; s += 64) ref = fmaxf(ref, p.part_ml[at + s].x);
-    ref = wave_max(ref);
-    float l = 0.f, o[2] = {0.f, 0.f};
-    const int dh = a.c.dh;
-    for (int s = 0; s < p.splits; ++s) {
-        const float2 ml = p.part_ml[at + s];
-        if (!(ml.y > 0.f)) continue;
-        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-        l += ml.y * f;
-        const float* x = p.part_o + (at + s) * dh;
-        if (lane < dh) o[0] += x[lane] * f;
-        if (lane + 64 < dh) o[1] += x[lane + 64] * f;
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const int lane = threadIdx.x & 63;
+    const Prefix pre = prefix_blocks(a, lane);
+    const int share = share_of(p, (long long)pre.total * a.c.n_kv);
+    long long start = lane_value(pre.before, b / pre.stretch);
+    for (int x = b / pre.stretch * pre.stretch; x < b; ++x) start += state_blocks(a, x);
+    const int blocks = (st.len + 31) >> 5;
+    start = start * a.c.n_kv + (long long)h * blocks;
     float* y = out_row(a, st, h, p.group, r);
-    if (lane < dh) y[lane] = o[0] * inv;
-    if (lane + 64 < dh) y[lane + 64] = o[1] * inv;
+    const int d = threadIdx.x % LANES * 4, part = threadIdx.x / LANES;
+    if (blocks == 0) {
+        if (part == 0 && d < DH) *reinterpret_cast<v4f*>(y + d) = v4f{0.f, 0.f, 0.f, 0.f};
+        if (p.lse && threadIdx.x == 0) p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + r] = INFINITY;
+        return;
+    }
+    const int w0 = (int)(start / share), w1 = (int)((start + blocks - 1) / share);
+    if (w0 == w1) return;                                              // written by that workgroup
+    auto slot = [&](int w) { return (2 * (size_t)w + (w == w0 && start > (long long)w * share ? 1 : 0)) * p.rows_pad + r; };
+    float ref = -INFINITY;
+    for (int w = w0 + lane; w <= w1; w += 64) ref = fmaxf(ref, p.part_ml[slot(w)].x);
+    ref = wave_max(ref);
+    float l = 0.f;
+    v4f o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int w = w0 + part; w <= w1; w += PARTS) {
+        const float2 ml = p.part_ml[slot(w)];
+        const v4f x = d < DH ? *reinterpret_cast<const v4f*>(p.part_o + slot(w) * DH + d) : v4f{0.f, 0.f, 0.f, 0.f};
+        const float f = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
+        l += ml.y * f;
+        o += x * f;
+    }
+    __shared__ float s_l[PARTS];
+    if (d < DH) *reinterpret_cast<v4f*>(&s_o[part][d]) = o;
+    if (d == 0) s_l[part] = l;
+    __syncthreads();
+    if (part != 0 || d >= DH) return;
+    l = 0.f;
+    o = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < PARTS; ++x) {
+        l += s_l[x];
+        o += *reinterpret_cast<const v4f*>(&s_o[x][d]);
+    }
+    *reinterpret_cast<v4f*>(y + d) = o * (l > 0.f ? 1.f / l : 0.f);
+    if (p.lse && d == 0) p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + r] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
 }
 
 // ---- weights of slots from the stored scores: a thread per four slots ----
 __global__ __launch_bounds__(256) void cached_weights_kernel(CachedAttention a, Plan p, int chunks) {
-    __shared__ float s_lse[32];
     const int h = blockIdx.x / chunks % a.c.n_kv, b = blockIdx.x / chunks / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
     const int rows = st.n * p.group, slot = (blockIdx.x % chunks * 256 + threadIdx.x) * 4;
     const size_t unit = ((size_t)b * a.c.n_kv + h) * p.rows_pad;
-    if (rows == 0) return;
-    if (threadIdx.x < 32 && (int)threadIdx.x < rows) {
-        float ref = -INFINITY, l = 0.f;
-        for (int s = 0; s < p.splits; ++s) ref = fmaxf(ref, p.part_ml[(unit + threadIdx.x) * p.splits + s].x);
-        for (int s = 0; s < p.splits; ++s) {
-            const float2 ml = p.part_ml[(unit + threadIdx.x) * p.splits + s];
-            if (ml.y > 0.f) l += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
-        }
-        s_lse[threadIdx.x] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
-    }
-    __syncthreads();
     if (slot >= st.len) return;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int r = 0; r < rows; ++r) {
         const float4 s = *reinterpret_cast<const float4*>(p.scores + (unit + r) * p.ld_scores + slot);
-        const float lse = s_lse[r];
+        const float lse = p.lse[unit + r];
         w[0] += __builtin_amdgcn_exp2f(s.x - lse);
         w[1] += __builtin_amdgcn_exp2f(s.y - lse);
         w[2] += __builtin_amdgcn_exp2f(s.z - lse);
@@ -734,7 +833,7 @@ int launch_simple(const CachedAttention& a, void* workspace, hipStream_t s) {
 struct Layout {
     Plan p;
     int waves, rt;
-    size_t o_off, ml_off, scores_off, total;
+    size_t o_off, ml_off, lse_off, scores_off, total;
 };
 
 Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int max_len, bool weights) {
@@ -744,38 +843,51 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
     p.group = n_heads / c.n_kv;
     p.rows_max = max_new * p.group;
     const int units = B * c.n_kv, blocks = (max_len + 31) / 32;
-    if (p.rows_max <= 32) {
-        L.rt = p.rows_max <= 16 ? 1 : 2;
-        p.row_blocks = 1;
-        L.waves = 4;
-        int s = (1536 + units - 1) / units;
-        const int most = (blocks + L.waves * 2 - 1) / (L.waves * 2);
-        if (s > most) s = most;
-        p.splits = s < 1 ? 1 : s;
-        p.rows_pad = L.rt * 16;
-        const size_t rows = (size_t)units * p.rows_pad;
-        size_t off = 0;
-        if (p.splits > 1) { L.o_off = off; off += round_up_sz(rows * p.splits * c.dh * 4, 256); }
-        if (p.splits > 1 || weights) { L.ml_off = off; off += round_up_sz(rows * p.splits * 8, 256); }
-        if (weights) {
-            p.ld_scores = (size_t)blocks * 32;
-            L.scores_off = off;
-            off += round_up_sz(rows * p.ld_scores * 4, 256);
-        }
-        L.total = off;
-    } else {
+    if (p.rows_max > 32) {
         L.total = weights ? (size_t)T * n_heads * 4 : 0;
+        return L;
     }
+    L.rt = p.rows_max <= 16 ? 1 : 2;
+    p.rows_pad = L.rt * 16;
+    // One workgroup of eight wavefronts per (state, k/v head) where that is a few blocks for each of them: no second launch.
+    if (blocks <= 32) {
+        L.waves = 8;
+    } else {
+        L.waves = 4;
+        p.groups = 512;
+        p.least = 8;
+    }
+    const size_t rows = (size_t)units * p.rows_pad, parts = 2 * (size_t)p.groups * p.rows_pad;
+    size_t off = 0;
+    if (p.groups) {
+        L.o_off = off; off += round_up_sz(parts * c.dh * 4, 256);
+        L.ml_off = off; off += round_up_sz(parts * 8, 256);
+    }
+    if (weights) {
+        L.lse_off = off; off += round_up_sz(rows * 4, 256);
+        p.ld_scores = (size_t)blocks * 32;
+        L.scores_off = off; off += round_up_sz(rows * p.ld_scores * 4, 256);
+    }
+    L.total = off;
     return L;
 }
 
 template <int DT, int DH>
 int launch_stream(const CachedAttention& a, const Layout& L, hipStream_t s) {
-    const dim3 grid((unsigned)(a.t.B * a.c.n_kv * L.p.splits)), block(L.waves * 64);
+    const dim3 grid((unsigned)(L.p.groups ? L.p.groups : a.t.B * a.c.n_kv)), block(L.waves * 64);
     const size_t lds = (size_t)L.waves * Shape<DT, DH>::LDS;
     if (L.rt == 1) hipLaunchKernelGGL((cached_stream_kernel<DT, DH, 1>), grid, block, lds, s, a, L.p);
     else hipLaunchKernelGGL((cached_stream_kernel<DT, DH, 2>), grid, block, lds, s, a, L.p);
     BRL_LAUNCH_CHECK("cached_stream_kernel");
+    if (L.p.groups) {
+        hipLaunchKernelGGL(cached_join_kernel<DH>, dim3((unsigned)(a.t.B * a.c.n_kv * L.p.rows_max)), dim3(256), 0, s, a, L.p);
+        BRL_LAUNCH_CHECK("cached_join_kernel");
+    }
+    if (a.weights) {
+        const int chunks = (a.t.max_len + 1023) / 1024;
+        hipLaunchKernelGGL(cached_weights_kernel, dim3((unsigned)(a.t.B * a.c.n_kv * chunks)), dim3(256), 0, s, a, L.p, chunks);
+        BRL_LAUNCH_CHECK("cached_weights_kernel");
+    }
     return BRL_OK;
 }
 
@@ -800,27 +912,18 @@ int launch_cached_attention(const CachedAttention& a, void* workspace, hipStream
     Layout L = plan_cached(a.c, a.n_heads, a.t.T, a.t.B, a.t.max_new, a.t.max_len, a.weights != nullptr);
     char* base = static_cast<char*>(workspace);
     LaunchTimer tm(BRL_KC_ATTENTION, s);
-    if (L.p.rows_max <= 32) {
-        Plan& p = L.p;
-        if (p.splits > 1) p.part_o = reinterpret_cast<float*>(base + L.o_off);
-        if (p.splits > 1 || a.weights) p.part_ml = reinterpret_cast<float2*>(base + L.ml_off);
-        if (a.weights) p.scores = reinterpret_cast<float*>(base + L.scores_off);
-        const int rc = a.c.dtype == BRL_F32 ? launch_stream_dh<BRL_F32>(a, L, s) : a.c.dtype == BRL_F16 ? launch_stream_dh<BRL_F16>(a, L, s)
-                                                                                                   : launch_stream_dh<BRL_I8>(a, L, s);
-        if (rc) return rc;
-        if (p.splits > 1) {
-            const long long rows = (long long)a.t.B * a.c.n_kv * p.rows_max;
-            hipLaunchKernelGGL(cached_join_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p);
-            BRL_LAUNCH_CHECK("cached_join_kernel");
-        }
-        if (a.weights) {
-            const int chunks = (a.t.max_len + 1023) / 1024;
-            hipLaunchKernelGGL(cached_weights_kernel, dim3((unsigned)(a.t.B * a.c.n_kv * chunks)), dim3(256), 0, s, a, p, chunks);
-            BRL_LAUNCH_CHECK("cached_weights_kernel");
-        }
-        return BRL_OK;
+    if (L.p.rows_max > 32) return launch_simple(a, workspace, s);
+    Plan& p = L.p;
+    if (p.groups) {
+        p.part_o = reinterpret_cast<float*>(base + L.o_off);
+        p.part_ml = reinterpret_cast<float2*>(base + L.ml_off);
     }
-    return launch_simple(a, workspace, s);
+    if (a.weights) {
+        p.lse = reinterpret_cast<float*>(base + L.lse_off);
+        p.scores = reinterpret_cast<float*>(base + L.scores_off);
+    }
+    return a.c.dtype == BRL_F32 ? launch_stream_dh<BRL_F32>(a, L, s) : a.c.dtype == BRL_F16 ? launch_stream_dh<BRL_F16>(a, L, s)
+                                                                                           : launch_stream_dh<BRL_I8>(a, L, s);
 }
 
 }  // namespace brl

@@ -248,11 +248,17 @@ struct KvView {
     const int32_t* table;     // [states][table_pages]
     int n_pages, page_shift, n_kv, dh, row, dtype, table_pages;
 };
-// Index of a slot's row in units of rows, -1 for a page number outside the pool: nothing is read or written there.
-__device__ __forceinline__ long long kv_row_index(const KvView& c, int b, int h, int slot) {
-    const int page = c.table[(size_t)b * c.table_pages + (slot >> c.page_shift)];
+// Index of a slot's row in units of rows (a pool has fewer than 2^31), -1 for a page number outside the pool: nothing is read
+// or written there.
+__device__ __forceinline__ int kv_page_row(const KvView& c, int page, int h, int slot) {
     if ((unsigned)page >= (unsigned)c.n_pages) return -1;
-    return (((long long)page * c.n_kv + h) << c.page_shift) + (slot & ((1 << c.page_shift) - 1));
+    return ((page * c.n_kv + h) << c.page_shift) + (slot & ((1 << c.page_shift) - 1));
+}
+__device__ __forceinline__ const int32_t* kv_table_entry(const KvView& c, int b, int slot) {
+    return c.table + ((size_t)b * c.table_pages + (slot >> c.page_shift));
+}
+__device__ __forceinline__ int kv_row_index(const KvView& c, int b, int h, int slot) {
+    return kv_page_row(c, *kv_table_entry(c, b, slot), h, slot);
 }
 // New tokens of the states of a call: rows row0 .. row0 + n - 1 of state b, in the slots base .. base + n - 1 of its cache.
 // Whatever the device arrays hold, rows stay inside [0, T) and slots inside the table (base may be negative: such tokens

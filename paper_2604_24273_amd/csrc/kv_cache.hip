@@ -57,7 +57,7 @@ __device__ __forceinline__ void store_elements(char* row, int d, const Floats<VW
 }
 
 template <int DT, int VW, int GS>
-__device__ __forceinline__ void store_row(char* pool, float* scales, long long idx, int rowlen, int dh, const Floats<VW>& a,
+__device__ __forceinline__ void store_row(char* pool, float* scales, int idx, int rowlen, int dh, const Floats<VW>& a,
                                           const Floats<VW>& b, int lane) {
     const int half = dh / 2;
     const bool mine = lane * VW < half;
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(AP_THREADS) void cache_append_kernel(AppendArgs a) 
     if (i >= st.n) return;                                        // (whole groups leave)
     const int slot = st.base + i;
     if (slot < 0) return;
-    const long long idx = kv_row_index(a.c, b, h, slot);
+    const int idx = kv_row_index(a.c, b, h, slot);
     if (idx < 0) return;
     const int row = st.row0 + i, pos = rope_position(a.t, row, slot);
     const int d = lane * VW < half ? lane * VW : 0;
@@ -256,11 +256,11 @@ __device__ __forceinline__ void move_rows(const CompactArgs& a, T* pool, size_t 
             if (item >= rows * units || r >= count) continue;
             const int src = kept[r], dst = start + r;
             if (src <= dst || src >= len) continue;
-            const long long from = paged ? kv_row_index(a.c, b, h, src) : src;
-            const long long at = paged ? kv_row_index(a.c, b, h, dst) : dst;
+            const int from = paged ? kv_row_index(a.c, b, h, src) : src;
+            const int at = paged ? kv_row_index(a.c, b, h, dst) : dst;
             if (from < 0 || at < 0) continue;
             v[e] = pool[(size_t)from * row_units + u];
-            to[e] = at * (long long)row_units + u;
+            to[e] = (long long)at * (long long)row_units + u;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // read, not only requested
         __syncthreads();

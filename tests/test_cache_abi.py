@@ -50,7 +50,7 @@ def test_caches_are_checked(B):
     for bad, word in ((dict(page_tokens=24), "page_tokens"), (dict(page_tokens=8), "page_tokens"), (dict(page_tokens=512), "page_tokens"),
                       (dict(n_kv_heads=0), "n_kv_heads"), (dict(head_dim=96), "head_dim"), (dict(dtype=B.BRL_BF16), "dtype"),
                       (dict(n_pages=0), "n_pages"), (dict(table_pages=0), "table_pages"), (dict(table_pages=1 << 30), "table_pages"),
-                      (dict(k=None), "null"), (dict(v=ODD), "misaligned"), (dict(page_table=None), "null"),
+                      (dict(n_pages=2 ** 25), "rows"), (dict(k=None), "null"), (dict(v=ODD), "misaligned"), (dict(page_table=None), "null"),
                       (dict(dtype=B.BRL_I8), "k_scale"), (dict(k_scale=FAKE), "k_scale"),
                       (dict(dtype=B.BRL_I8, k_scale=FAKE), "v_scale")):
         assert append(cache(B, **bad)) == B.BRL_EINVAL and word in err(), bad
