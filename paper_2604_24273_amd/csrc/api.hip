@@ -1006,7 +1006,7 @@ int check_new_tokens(const KvView& v, const float* qkv, int n_heads, int T, int 
     BRL_REQUIRE(rope_len >= 1, "%s: rope_len = %d", who, rope_len);
     if (max_new > T) max_new = T;
     // workgroups and items of a launch are counted in 32 bits
-    BRL_REQUIRE((long long)max_new * n_heads * B <= (1ll << 30) && (long long)B * n_heads <= (1 << 22),
+    BRL_REQUIRE((long long)max_new * n_heads * B <= (1ll << 26) && (long long)B * n_heads <= (1 << 22),
                 "%s: too much for one call (max_new %d, B %d, n_heads %d)", who, max_new, B, n_heads);
     t.cu = cu_new; t.lens = lens; t.pos = positions;
     t.cos_t = rope_cos; t.sin_t = rope_sin;
@@ -1067,6 +1067,8 @@ int attention_cached_forward(const brl_kv_cache* cache, const float* qkv, int n_
     BRL_REQUIRE((tree_mask == nullptr) == (mask_words == 0) && mask_words >= 0 && mask_words <= KV_MAX_TOKENS / 32,
                 "%s: mask_words = %d", who, mask_words);
     BRL_REQUIRE(!weights || ld_weights >= max_len, "%s: ld_weights = %d below max_len = %d", who, ld_weights, max_len);
+    BRL_REQUIRE(!weights || (long long)B * a.c.n_kv * max_len <= (1ll << 30), "%s: too many weights for one call (B %d, n_kv_heads %d, max_len %d)",
+                who, B, a.c.n_kv, max_len);
     const size_t need = brl_attention_cached_workspace_bytes(cache, n_heads, T, B, max_new, max_len, weights != nullptr);
     if (ws_bytes < need) {
         set_error("%s: workspace %zu < %zu", who, ws_bytes, need);

@@ -209,15 +209,14 @@ struct ValueReads {
     }
 };
 
-// Query rows, rotated, scaled and split, as operand fragments in LDS: [row tile][step][hi, lo][64 lanes] of 16 bytes; lane
-// 16 g + c of a fragment holds components 32 s + 8 g .. of row c.  A job is one lane of one (row tile, step).
+// Eight components d0 .. of a query row, rotated, scaled and split into an operand's hi and lo words.  Fragments hold, in lane
+// 16 g + c, components 32 s + 8 g .. of row c.
 template <class S>
-struct QueryJob {
+struct QueryPart {
     float x[8], y[8], c[8], w[8];      // components, their partners, cosines, sines
-    __device__ __forceinline__ void request(const CachedAttention& a, const StateTokens& st, int h, int group, int rows, int job) {
+    __device__ __forceinline__ void request(const CachedAttention& a, const StateTokens& st, int h, int group, int r, int d0) {
         constexpr int DH = S::DH, half = DH / 2;
-        const int lane = job & 63, s = (job >> 6) % S::KS, r0 = (job >> 6) / S::KS * 16 + (lane & 15), r = r0 < rows ? r0 : rows - 1;
-        const int i = r / group, row = st.row0 + i, pos = rope_position(a.t, row, st.base + i), d0 = 32 * s + 8 * (lane >> 4);
+        const int i = r / group, row = st.row0 + i, pos = rope_position(a.t, row, st.base + i);
         const float* q = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * DH) + (h * group + r % group) * DH;
         const float *ct = a.t.cos_t + (size_t)pos * half, *sn = a.t.sin_t + (size_t)pos * half;
         if constexpr (DH % 16 == 0) {                                  // eight components lie in one half
@@ -237,22 +236,35 @@ struct QueryJob {
             }
         }
     }
-    __device__ __forceinline__ void store(uint4* lds, int rows, int job) const {
+    __device__ __forceinline__ void split(bool live, int d0, uint4& hi, uint4& lo) const {
         constexpr int DH = S::DH, half = DH / 2;
         const float scale = (float)(1.0 / sqrt((double)DH)) * LOG2E;
-        const int lane = job & 63, s = (job >> 6) % S::KS, rt = (job >> 6) / S::KS, d0 = 32 * s + 8 * (lane >> 4);
-        const bool live = rt * 16 + (lane & 15) < rows;
-        uint32_t hi[4], lo[4];
         float z[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float p = y[e] * w[e];
             z[e] = live && d0 + e < DH ? (x[e] * c[e] + (d0 + e < half ? -p : p)) * scale : 0.f;
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) split_pair(z[2 * e], z[2 * e + 1], hi[e], lo[e]);
-        lds[((rt * S::KS + s) * 2) * 64 + lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        lds[((rt * S::KS + s) * 2 + 1) * 64 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        split_pair(z[0], z[1], hi.x, lo.x);
+        split_pair(z[2], z[3], hi.y, lo.y);
+        split_pair(z[4], z[5], hi.z, lo.z);
+        split_pair(z[6], z[7], hi.w, lo.w);
+    }
+};
+// The same as a job: one lane of one (row tile, step) of fragments in LDS, [row tile][step][hi, lo][64 lanes].
+template <class S>
+struct QueryJob {
+    QueryPart<S> part;
+    __device__ __forceinline__ void request(const CachedAttention& a, const StateTokens& st, int h, int group, int rows, int job) {
+        const int lane = job & 63, r = (job >> 6) / S::KS * 16 + (lane & 15);
+        part.request(a, st, h, group, r < rows ? r : rows - 1, 32 * ((job >> 6) % S::KS) + 8 * (lane >> 4));
+    }
+    __device__ __forceinline__ void store(uint4* lds, int rows, int job) const {
+        const int lane = job & 63, s = (job >> 6) % S::KS, rt = (job >> 6) / S::KS;
+        uint4 hi, lo;
+        part.split(rt * 16 + (lane & 15) < rows, 32 * s + 8 * (lane >> 4), hi, lo);
+        lds[((rt * S::KS + s) * 2) * 64 + lane] = hi;
+        lds[((rt * S::KS + s) * 2 + 1) * 64 + lane] = lo;
     }
 };
 
@@ -362,6 +374,8 @@ __device__ __forceinline__ void block_values(const char* lds, const float (&p)[R
 
 struct Plan {
     int group, rows_max;      // query heads per k/v head; rows of a state at most
+    int row_blocks, splits;   // many rows: blocks of rows of a (state, k/v head), parts of the keys
+    uint4* q;                 // many rows with weights: [B][n_kv][rows_pad / 16][steps][hi, lo][64] query fragments
     int rows_pad;             // rows reserved per (state, k/v head) in the scratch space
     int groups;               // workgroups that share all blocks evenly, 0: one workgroup per (state, k/v head)
     int least;                // blocks a workgroup takes at least
@@ -723,117 +737,368 @@ __global__ __launch_bounds__(256) void cached_weights_kernel(CachedAttention a, 
         if (slot + e < st.len) y[e] += w[e];
 }
 
-// element d of a row of the cache, widened
-__device__ __forceinline__ float cache_value(const char* pool, const float* scales, int dtype, int row, long long idx, int d) {
-    const size_t e = (size_t)idx * row + d;
-    if (dtype == BRL_F32) return reinterpret_cast<const float*>(pool)[e];
-    if (dtype == BRL_F16) return (float)reinterpret_cast<const _Float16*>(pool)[e];
-    return (float)reinterpret_cast<const int8_t*>(pool)[e] * scales[idx];
-}
-
-__device__ __forceinline__ bool sees(const CachedAttention& a, const StateTokens& st, int i, int slot) {
-    if (!a.tree) return slot <= st.base + i;
-    const int j = slot - st.base;
-    if (j < 0) return true;
-    return (j >> 5) < a.mask_words && (a.tree[(size_t)(st.row0 + i) * a.mask_words + (j >> 5)] >> (j & 31) & 1u);
-}
-
-// One wavefront per token and query head; a lane per slot for the scores, per component for the sum.
-__global__ __launch_bounds__(64) void cached_rows_kernel(CachedAttention a, float* lse) {
-    __shared__ float q[128], p[64];
-    __shared__ long long rows[64];
-    const int lane = threadIdx.x, hq = blockIdx.x % a.n_heads;
-    const int b = blockIdx.x / a.n_heads / a.t.max_new, i = blockIdx.x / a.n_heads % a.t.max_new;
-    const StateTokens st = state_tokens(a.t, a.c, b);
-    if (i >= st.n) return;
-    const int dh = a.c.dh, half = dh / 2, h = hq / (a.n_heads / a.c.n_kv), row = st.row0 + i;
-    const float* x = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * dh) + hq * dh;
-    const int pos = rope_position(a.t, row, st.base + i);
-    const float scale = (float)(1.0 / sqrt((double)dh)) * 1.4426950408889634f;
-    if (lane < half) {
-        const float c = a.t.cos_t[(size_t)pos * half + lane], s = a.t.sin_t[(size_t)pos * half + lane];
-        q[lane] = (x[lane] * c - x[lane + half] * s) * scale;
-        q[lane + half] = (x[lane + half] * c + x[lane] * s) * scale;
+// ---- many rows: the wavefronts of a workgroup share every block of keys and values through LDS ----
+// A wavefront owns RT tiles of 16 rows, whose operands stay in its registers.  While a block is worked on, the next one is on its way
+// into registers; it goes to the other half of LDS at the end, so that one barrier per block is enough.
+template <class S>
+struct SharedLoads {
+    static constexpr int N = (32 * S::CPR + 255) / 256;
+    uint4 k[N], v[N];
+    float scale;
+    __device__ __forceinline__ void request(const KvView& c, int lo, int hi, int tid) {
+        const size_t lo_at = (size_t)(lo < 0 ? 0 : lo) * S::RB, hi_at = (size_t)(hi < 0 ? 0 : hi) * S::RB;
+        constexpr int HALF = 16 * S::CPR;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int idx = i * 256 + tid;
+            if (N * 256 > 32 * S::CPR && idx >= 32 * S::CPR) continue;
+            const size_t at = idx >= HALF ? hi_at + (size_t)((idx - HALF) * 16) : lo_at + (size_t)(idx * 16);
+            k[i] = *reinterpret_cast<const uint4*>(c.k + at);
+            v[i] = *reinterpret_cast<const uint4*>(c.v + at);
+        }
+        if constexpr (S::DT == BRL_I8) {
+            const int key = tid & 31, r = key < 16 ? lo : hi;
+            scale = (tid & 32 ? c.vs : c.ks)[(r < 0 ? 0 : r) + (key & 15)];
+        }
     }
+    // there: bit per key whose row holds numbers
+    __device__ __forceinline__ void store(char* lds, float* scales, int tid, uint32_t there) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int idx = i * 256 + tid, key = idx / S::CPR, ch = idx % S::CPR;
+            if (N * 256 > 32 * S::CPR && idx >= 32 * S::CPR) continue;
+            uint4 x = k[i], y = v[i];
+            if (there != 0xffffffffu && !(there >> key & 1u)) y = make_uint4(0, 0, 0, 0);
+            if constexpr (S::ROW > S::DH) {                            // what lies behind head_dim is not a number
+                constexpr int PER = 16 / S::SZ;
+                const int valid = S::DH - ch * PER;                    // elements of this chunk
+                uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = j * (4 / S::SZ) < valid ? w[j] : 0u;
+                x = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            put(lds, key, ch, x);
+            put(lds + S::LDS, key, ch, y);
+        }
+        if constexpr (S::DT == BRL_I8) {
+            if (tid < 64) scales[tid] = there >> (tid & 31) & 1u ? scale : 0.f;
+        }
+    }
+    static __device__ __forceinline__ void put(char* lds, int key, int ch, const uint4& r) {
+        if constexpr (S::DT == BRL_F16) {
+            *reinterpret_cast<uint4*>(lds + lds_chunk<S>(key, ch)) = r;
+        } else if constexpr (S::DT == BRL_F32) {
+            uint2 h, l;
+            split_pair(__uint_as_float(r.x), __uint_as_float(r.y), h.x, l.x);
+            split_pair(__uint_as_float(r.z), __uint_as_float(r.w), h.y, l.y);
+            char* p = lds + lds_chunk<S>(key, ch >> 1) + (ch & 1) * 8;
+            *reinterpret_cast<uint2*>(p) = h;
+            *reinterpret_cast<uint2*>(p + S::PLANE) = l;
+        } else {
+            uint4 a, b;
+            widen_codes(r.x, a.x, a.y);
+            widen_codes(r.y, a.z, a.w);
+            widen_codes(r.z, b.x, b.y);
+            widen_codes(r.w, b.z, b.w);
+            *reinterpret_cast<uint4*>(lds + lds_chunk<S>(key, 2 * ch)) = a;
+            *reinterpret_cast<uint4*>(lds + lds_chunk<S>(key, 2 * ch + 1)) = b;
+        }
+    }
+};
+
+// the slots that rows r0 .. r1 of a state can see at all end here
+__device__ __forceinline__ int end_of_sight(const CachedAttention& a, const StateTokens& st, int group, int r1) {
+    const int n = a.tree ? st.len : st.base + r1 / group + 1;
+    return n < 0 ? 0 : n;
+}
+
+template <int DT, int DH, int RT>
+__global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a, Plan p) {
+    typedef Shape<DT, DH> S;
+    constexpr int ROWS = 64 * RT;                                      // of a workgroup
+    __shared__ __attribute__((aligned(16))) char s_kv[2][2 * S::LDS];   // keys, values; two blocks
+    __shared__ float s_scale[2][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    // blocks of rows from the last to the first: with causal masks the last see most keys
+    const int units = a.t.B * a.c.n_kv, unit = blockIdx.x % units, split = blockIdx.x / units % p.splits;
+    const int rb = p.row_blocks - 1 - (int)(blockIdx.x / units) / p.splits, h = unit % a.c.n_kv, b = unit / a.c.n_kv;
+    const StateTokens st = state_tokens(a.t, a.c, b);
+    const int rows = st.n * p.group, r0 = rb * ROWS;
+    if (r0 >= rows) return;
+    const int r1 = (r0 + ROWS < rows ? r0 + ROWS : rows) - 1;
+    const int blocks = (end_of_sight(a, st, p.group, r1) + 31) >> 5, per = (blocks + p.splits - 1) / p.splits;
+    const int first = split * per, last = first + per < blocks ? first + per : blocks;
+
+    int page_lo = -1, page_hi = -1;
+    auto pages = [&](int t0) {
+        const int slot = (t0 + lane) * 32;
+        page_lo = slot < st.len ? kv_row_index(a.c, b, h, slot) : -1;
+        page_hi = slot + 16 < st.len ? kv_row_index(a.c, b, h, slot + 16) : -1;
+    };
+    auto there_of = [&](int t, int lo, int hi) {
+        const int n = st.len - t * 32;
+        uint32_t x = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+        if (lo < 0) x &= 0xffff0000u;
+        if (hi < 0) x &= 0x0000ffffu;
+        return x;
+    };
+    SharedLoads<S> load;
+    int lo = -1, hi = -1;
+    if (first < last) {
+        pages(first);
+        lo = lane_value(page_lo, 0);
+        hi = lane_value(page_hi, 0);
+        load.request(a.c, lo, hi, tid);
+    }
+    // this wavefront's rows
+    const int w0 = r0 + wave * 16 * RT, w1 = w0 + 16 * RT - 1 < r1 ? w0 + 16 * RT - 1 : r1;
+    const bool busy = w0 <= r1;
+    const int wave_blocks = busy ? (end_of_sight(a, st, p.group, w1) + 31) >> 5 : 0;
+    const int all_see = st.base + (a.tree ? 0 : w0 / p.group + 1);
+    RowState<S> row[RT];
+    v8h qh[RT][S::KS], ql[RT][S::KS];
+    int token[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        row[r].clear();
+        const int rr = w0 + r * 16 + c;
+        token[r] = (rr < rows ? rr : rows - 1) / p.group;
+#pragma unroll
+        for (int s = 0; s < S::KS; ++s) {
+            QueryPart<S> q;
+            q.request(a, st, h, p.group, rr < rows ? rr : rows - 1, 32 * s + 8 * g);
+            uint4 x, y;
+            q.split(rr < rows, 32 * s + 8 * g, x, y);
+            qh[r][s] = __builtin_bit_cast(v8h, x);
+            ql[r][s] = __builtin_bit_cast(v8h, y);
+            if (p.q && split == 0 && w0 + r * 16 <= r1) {
+                uint4* f = p.q + ((((size_t)unit * p.rows_pad + w0 + r * 16) / 16 * S::KS + s) * 2) * 64 + lane;
+                f[0] = x;
+                f[64] = y;
+            }
+        }
+    }
+    if constexpr (S::NCH * 8 > S::ROW) {                               // components of the last step that no row has
+        for (int i = tid; i < 2 * S::PL * 32 * (S::NCH - S::ROW / 8); i += 256) {
+            const int x = i % (S::NCH - S::ROW / 8), key = i / (S::NCH - S::ROW / 8) % 32, plane = i / (S::NCH - S::ROW / 8) / 32;
+            *reinterpret_cast<uint4*>(s_kv[plane / S::PL] + plane % S::PL * S::PLANE + lds_chunk<S>(key, S::ROW / 8 + x)) = make_uint4(0, 0, 0, 0);
+        }
+    }
+    float unit_scale = 0x1p126f;                                       // int8: power of two that the sums are multiplied by
+    if (first < last) load.store(s_kv[0], s_scale[0], tid, there_of(first, lo, hi));
     __syncthreads();
-    float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int k0 = 0; k0 < st.len; k0 += 64) {
-        const int slot = k0 + lane;
-        const long long idx = slot < st.len ? kv_row_index(a.c, b, h, slot) : -1;
-        float v = -INFINITY;
-        if (idx >= 0 && sees(a, st, i, slot)) {
-            v = 0.f;
-            for (int d = 0; d < dh; ++d) v += q[d] * cache_value(a.c.k, a.c.ks, a.c.dtype, a.c.row, idx, d);
+    int ahead = 0, buf = 0;
+    for (int t = first; t < last; ++t) {
+        if (++ahead == 64) {
+            ahead = 0;
+            pages(t + 1);
         }
-        const float m_new = fmaxf(m, wave_max(v));
-        if (m_new == -INFINITY) continue;
-        const float e = __builtin_amdgcn_exp2f(v - m_new), alpha = __builtin_amdgcn_exp2f(m - m_new);
-        p[lane] = e;
-        rows[lane] = e > 0.f ? idx : -1;
-        __syncthreads();
-        l = l * alpha + wave_total(e);
-        o0 *= alpha; o1 *= alpha;
-        for (int k = 0; k < 64; ++k) {
-            if (rows[k] < 0) continue;
-            if (lane < dh) o0 += p[k] * cache_value(a.c.v, a.c.vs, a.c.dtype, a.c.row, rows[k], lane);
-            if (lane + 64 < dh) o1 += p[k] * cache_value(a.c.v, a.c.vs, a.c.dtype, a.c.row, rows[k], lane + 64);
+        const bool more = t + 1 < last;
+        const int next_lo = more ? lane_value(page_lo, ahead) : -1, next_hi = more ? lane_value(page_hi, ahead) : -1;
+        load.request(a.c, next_lo, next_hi, tid);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t < wave_blocks) {
+            const char* keys = s_kv[buf];
+            const char* vals = keys + S::LDS;
+            float s[RT][8];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                v4f acc[RT];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) acc[r] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < S::KS; ++x) {
+                    const char* f = keys + lds_chunk<S>(8 * (c >> 2) + 4 * kt + (c & 3), (4 * x + g) & (S::NCH - 1));
+                    const v8h kh = __builtin_bit_cast(v8h, *reinterpret_cast<const uint4*>(f));
+                    v8h kl;
+                    if constexpr (S::PL == 2) kl = __builtin_bit_cast(v8h, *reinterpret_cast<const uint4*>(f + S::PLANE));
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        if constexpr (S::PL == 2) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qh[r][x], acc[r], 0, 0, 0);
+                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, ql[r][x], acc[r], 0, 0, 0);
+                        acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qh[r][x], acc[r], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[r][4 * kt + j] = acc[r][j];
+            }
+            float vf[8];
+            if constexpr (DT == BRL_I8) {
+                float kf[8];
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    *reinterpret_cast<float4*>(kf + e) = *reinterpret_cast<const float4*>(&s_scale[buf][8 * g + e]);
+                    *reinterpret_cast<float4*>(vf + e) = *reinterpret_cast<const float4*>(&s_scale[buf][32 + 8 * g + e]);
+                }
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[r][e] *= kf[e];
+            }
+            if (t * 32 + 32 > all_see || lo < 0 || hi < 0) {
+                const uint32_t mine = there_of(t, lo, hi) >> (8 * g) & 0xffu;
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    const uint32_t bits = mine & visible_bits(a, st, token[r], t * 32 + 8 * g);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[r][e] = bits >> e & 1u ? s[r][e] : -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) row[r].probabilities(s[r]);
+            if constexpr (DT == BRL_I8) {
+                float top = vf[0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) top = fmaxf(top, vf[e]);
+                if (__any(top * unit_scale > 1.f)) {
+                    const float now = __builtin_amdgcn_exp2f(-ceilf(__builtin_amdgcn_logf(wave_max(top))) - 1.f);
+                    const float f = now / unit_scale;
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) row[r].scale(f);
+                    unit_scale = now;
+                }
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[r][e] *= vf[e] * unit_scale;
+            }
+            block_values<S, RT>(vals, s, row, lane);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        load.store(s_kv[buf ^ 1], s_scale[buf ^ 1], tid, more ? there_of(t + 1, next_lo, next_hi) : 0u);
+        lo = next_lo;
+        hi = next_hi;
+        buf ^= 1;
         __syncthreads();
-        m = m_new;
+    }
+    if (!busy) return;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        float l = row[r].l;
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        const int rr = w0 + r * 16 + c;
+        if (rr > r1) continue;
+        float f = DT == BRL_I8 ? 1.f / unit_scale : 1.f;
+        float* y;
+        if (p.splits == 1) {
+            f *= l > 0.f ? 1.f / l : 0.f;
+            y = out_row(a, st, h, p.group, rr);
+            if (p.lse && g == 0) p.lse[(size_t)unit * p.rows_pad + rr] = l > 0.f ? row[r].ref + __builtin_amdgcn_logf(l) : INFINITY;
+        } else {
+            const size_t at = ((size_t)unit * p.rows_pad + rr) * p.splits + split;
+            y = p.part_o + at * DH;
+            if (g == 0) p.part_ml[at] = make_float2(l > 0.f ? row[r].ref : -INFINITY, l);
+        }
+#pragma unroll
+        for (int d = 0; d < S::DTL; ++d)
+            if (16 * d + 4 * g < DH) *reinterpret_cast<v4f*>(y + 16 * d + 4 * g) = row[r].o[d] * f;
+    }
+}
+
+// the parts of a row that a fixed number of workgroups took
+template <int DH>
+__global__ __launch_bounds__(64) void cached_join_splits_kernel(CachedAttention a, Plan p) {
+    const int lane = threadIdx.x, r = blockIdx.x % p.rows_max, unit = blockIdx.x / p.rows_max, h = unit % a.c.n_kv, b = unit / a.c.n_kv;
+    const StateTokens st = state_tokens(a.t, a.c, b);
+    if (r >= st.n * p.group) return;
+    const size_t at = ((size_t)unit * p.rows_pad + r) * p.splits;
+    float ref = -INFINITY;
+    for (int s = 0; s < p.splits; ++s) ref = fmaxf(ref, p.part_ml[at + s].x);
+    float l = 0.f, o[2] = {0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) {
+        const float2 ml = p.part_ml[at + s];
+        const float f = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
+        const float* x = p.part_o + (at + s) * DH;
+        l += ml.y * f;
+        if (lane < DH) o[0] += x[lane] * f;
+        if (DH > 64 && lane + 64 < DH) o[1] += x[lane + 64] * f;
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    float* o = a.out + (size_t)row * a.n_heads * dh + hq * dh;
-    if (lane < dh) o[lane] = o0 * inv;
-    if (lane + 64 < dh) o[lane + 64] = o1 * inv;
-    if (lse && lane == 0) lse[(size_t)row * a.n_heads + hq] = l > 0.f ? m + __builtin_amdgcn_logf(l) : INFINITY;
+    float* y = out_row(a, st, h, p.group, r);
+    if (lane < DH) y[lane] = o[0] * inv;
+    if (DH > 64 && lane + 64 < DH) y[lane + 64] = o[1] * inv;
+    if (p.lse && lane == 0) p.lse[(size_t)unit * p.rows_pad + r] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
 }
 
-// One thread per slot and k/v head: its weight summed over the rows that see it.
-__global__ __launch_bounds__(64) void simple_weights_kernel(CachedAttention a, const float* lse, int chunks) {
-    __shared__ float q[128];
-    const int lane = threadIdx.x, h = blockIdx.x / chunks % a.c.n_kv, b = blockIdx.x / chunks / a.c.n_kv;
-    const int slot = blockIdx.x % chunks * 64 + lane;
+// Weights of slots, many rows: the scores once more.  A wavefront keeps a block of 32 keys in registers and walks the row tiles that
+// can see it; each lane sums its eight keys over its row of every tile, the sixteen rows meet at the end.
+template <int DT, int DH>
+__global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAttention a, Plan p, int chunks) {
+    typedef Shape<DT, DH> S;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int unit = blockIdx.x / chunks, h = unit % a.c.n_kv, b = unit / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
-    const int dh = a.c.dh, half = dh / 2, group = a.n_heads / a.c.n_kv;
-    const float scale = (float)(1.0 / sqrt((double)dh)) * 1.4426950408889634f;
-    const long long idx = slot < st.len ? kv_row_index(a.c, b, h, slot) : -1;
-    float sum = 0.f;
-    for (int i = 0; i < st.n; ++i)
-        for (int g = 0; g < group; ++g) {
-            const int row = st.row0 + i, hq = h * group + g;
-            const float* x = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * dh) + hq * dh;
-            const int pos = rope_position(a.t, row, st.base + i);
-            __syncthreads();
-            if (lane < half) {
-                const float c = a.t.cos_t[(size_t)pos * half + lane], s = a.t.sin_t[(size_t)pos * half + lane];
-                q[lane] = (x[lane] * c - x[lane + half] * s) * scale;
-                q[lane + half] = (x[lane + half] * c + x[lane] * s) * scale;
-            }
-            __syncthreads();
-            if (idx < 0 || !sees(a, st, i, slot)) continue;
-            float v = 0.f;
-            for (int d = 0; d < dh; ++d) v += q[d] * cache_value(a.c.k, a.c.ks, a.c.dtype, a.c.row, idx, d);
-            sum += __builtin_amdgcn_exp2f(v - lse[(size_t)row * a.n_heads + hq]);
-        }
-    if (idx >= 0) a.weights[((size_t)b * a.c.n_kv + h) * a.ld_weights + slot] += sum;
-}
-
-int launch_simple(const CachedAttention& a, void* workspace, hipStream_t s) {
-    float* lse = a.weights ? static_cast<float*>(workspace) : nullptr;
-    hipLaunchKernelGGL(cached_rows_kernel, dim3((unsigned)a.t.B * a.t.max_new * a.n_heads), dim3(64), 0, s, a, lse);
-    if (a.weights) {
-        const int chunks = (a.t.max_len + 63) / 64;
-        hipLaunchKernelGGL(simple_weights_kernel, dim3((unsigned)a.t.B * a.c.n_kv * chunks), dim3(64), 0, s, a, (const float*)lse, chunks);
+    const int rows = st.n * p.group, slot0 = (blockIdx.x % chunks * 4 + wave) * 32;
+    if (rows == 0 || slot0 >= st.len) return;
+    const int lo = kv_row_index(a.c, b, h, slot0), hi = slot0 + 16 < st.len ? kv_row_index(a.c, b, h, slot0 + 16) : -1;
+    const int n = st.len - slot0;
+    uint32_t there = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+    if (lo < 0) there &= 0xffff0000u;
+    if (hi < 0) there &= 0x0000ffffu;
+    if (there == 0) return;
+    KeyLoads<S> raw;
+    raw.request(a.c.k, lo, hi, lane);
+    float kf[8];
+    if constexpr (DT == BRL_I8) {
+        const int r = (g >> 1) ? hi : lo;
+        const float* f = a.c.ks + (r < 0 ? 0 : r) + (g & 1) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) kf[e] = f[e];
     }
-    BRL_LAUNCH_CHECK("cached_rows_kernel");
-    return BRL_OK;
+    v8h key[2][S::KS][S::PL];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int s = 0; s < S::KS; ++s) raw.fragment(t, s, lane, key[t][s]);
+    const uint32_t mine = there >> (8 * g) & 0xffu;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int token0 = a.tree || slot0 <= st.base ? 0 : slot0 - st.base;          // the first token that sees the block's first slot
+    for (int rt = token0 * p.group / 16; rt * 16 < rows; ++rt) {
+        const uint4* q = p.q + (((size_t)unit * p.rows_pad / 16 + rt) * S::KS * 2) * 64 + lane;
+        const int r = rt * 16 + c;
+        const float lse = r < rows ? p.lse[(size_t)unit * p.rows_pad + r] : INFINITY;
+        v4f acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int s = 0; s < S::KS; ++s) {
+            const v8h qh = __builtin_bit_cast(v8h, q[s * 128]), ql = __builtin_bit_cast(v8h, q[s * 128 + 64]);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if constexpr (S::PL == 2) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[t][s][1], qh, acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[t][s][0], ql, acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[t][s][0], qh, acc[t], 0, 0, 0);
+            }
+        }
+        const int token = (r < rows ? r : rows - 1) / p.group;
+        uint32_t bits = mine;
+        if (slot0 + 32 > st.base + (a.tree ? 0 : rt * 16 / p.group + 1)) bits &= visible_bits(a, st, token, slot0 + 8 * g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = acc[e >> 2][e & 3];
+            if constexpr (DT == BRL_I8) x *= kf[e];
+            sum[e] += bits >> e & 1u ? __builtin_amdgcn_exp2f(x - lse) : 0.f;
+        }
+    }
+    float* y = a.weights + (size_t)unit * a.ld_weights + slot0 + 8 * g;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float x = sum[e];
+        x += lane_exchange<DPP_XOR1>(x);
+        x += lane_exchange<DPP_XOR2>(x);
+        x += lane_exchange<DPP_HALF_MIRROR>(x);
+        x += lane_exchange<DPP_MIRROR>(x);
+        if (c == 0 && mine >> e & 1u) y[e] += x;
+    }
 }
-
 
 struct Layout {
     Plan p;
-    int waves, rt;
-    size_t o_off, ml_off, lse_off, scores_off, total;
+    int waves, rt;            // few rows: wavefronts of a workgroup; row tiles of a wavefront
+    bool tiles;               // many rows
+    size_t o_off, ml_off, lse_off, scores_off, q_off, total;
 };
 
 Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int max_len, bool weights) {
@@ -842,63 +1107,103 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
     Plan& p = L.p;
     p.group = n_heads / c.n_kv;
     p.rows_max = max_new * p.group;
+    p.splits = 1;
     const int units = B * c.n_kv, blocks = (max_len + 31) / 32;
-    if (p.rows_max > 32) {
-        L.total = weights ? (size_t)T * n_heads * 4 : 0;
-        return L;
-    }
-    L.rt = p.rows_max <= 16 ? 1 : 2;
-    p.rows_pad = L.rt * 16;
-    // One workgroup of eight wavefronts per (state, k/v head) where that is a few blocks for each of them: no second launch.
-    if (blocks <= 32) {
-        L.waves = 8;
+    L.tiles = p.rows_max > 32;
+    size_t parts;
+    if (!L.tiles) {
+        L.rt = p.rows_max <= 16 ? 1 : 2;
+        p.rows_pad = L.rt * 16;
+        // One workgroup of eight wavefronts per (state, k/v head) where that is a few blocks for each of them: no second launch.
+        // So, too, where there are far more of them than workgroups at a time.
+        if (blocks <= 32 || (long long)units * p.rows_max > (1 << 22)) {
+            L.waves = 8;
+        } else {
+            L.waves = 4;
+            p.groups = 512;
+            p.least = 8;
+        }
+        parts = 2 * (size_t)p.groups * p.rows_pad;
     } else {
-        L.waves = 4;
-        p.groups = 512;
-        p.least = 8;
+        L.rt = p.rows_max <= 64 ? 1 : 2;
+        p.row_blocks = (p.rows_max + 64 * L.rt - 1) / (64 * L.rt);
+        p.rows_pad = p.row_blocks * 64 * L.rt;
+        const long long groups = (long long)units * p.row_blocks;
+        long long s = (1024 + groups - 1) / groups;
+        if (s > blocks / 8) s = blocks / 8;
+        p.splits = s < 1 ? 1 : (int)s;
+        parts = p.splits > 1 ? (size_t)units * p.rows_pad * p.splits : 0;
     }
-    const size_t rows = (size_t)units * p.rows_pad, parts = 2 * (size_t)p.groups * p.rows_pad;
+    const size_t rows = (size_t)units * p.rows_pad;
     size_t off = 0;
-    if (p.groups) {
-        L.o_off = off; off += round_up_sz(parts * c.dh * 4, 256);
-        L.ml_off = off; off += round_up_sz(parts * 8, 256);
-    }
+    auto take = [&off](size_t bytes) {
+        const size_t at = off;
+        off += round_up_sz(bytes, 256);
+        return at;
+    };
+    L.o_off = take(parts * c.dh * 4);
+    L.ml_off = take(parts * 8);
     if (weights) {
-        L.lse_off = off; off += round_up_sz(rows * 4, 256);
-        p.ld_scores = (size_t)blocks * 32;
-        L.scores_off = off; off += round_up_sz(rows * p.ld_scores * 4, 256);
+        L.lse_off = take(rows * 4);
+        if (L.tiles) {
+            L.q_off = take(rows * ((c.dh + 31) / 32) * 32 * 4);
+        } else {
+            p.ld_scores = (size_t)blocks * 32;
+            L.scores_off = take(rows * p.ld_scores * 4);
+        }
     }
     L.total = off;
     return L;
 }
 
 template <int DT, int DH>
-int launch_stream(const CachedAttention& a, const Layout& L, hipStream_t s) {
-    const dim3 grid((unsigned)(L.p.groups ? L.p.groups : a.t.B * a.c.n_kv)), block(L.waves * 64);
+int launch_few(const CachedAttention& a, const Layout& L, hipStream_t s) {
+    const Plan& p = L.p;
+    const dim3 grid((unsigned)(p.groups ? p.groups : a.t.B * a.c.n_kv)), block(L.waves * 64);
     const size_t lds = (size_t)L.waves * Shape<DT, DH>::LDS;
-    if (L.rt == 1) hipLaunchKernelGGL((cached_stream_kernel<DT, DH, 1>), grid, block, lds, s, a, L.p);
-    else hipLaunchKernelGGL((cached_stream_kernel<DT, DH, 2>), grid, block, lds, s, a, L.p);
+    if (L.rt == 1) hipLaunchKernelGGL((cached_stream_kernel<DT, DH, 1>), grid, block, lds, s, a, p);
+    else hipLaunchKernelGGL((cached_stream_kernel<DT, DH, 2>), grid, block, lds, s, a, p);
     BRL_LAUNCH_CHECK("cached_stream_kernel");
-    if (L.p.groups) {
-        hipLaunchKernelGGL(cached_join_kernel<DH>, dim3((unsigned)(a.t.B * a.c.n_kv * L.p.rows_max)), dim3(256), 0, s, a, L.p);
+    if (p.groups) {
+        hipLaunchKernelGGL(cached_join_kernel<DH>, dim3((unsigned)(a.t.B * a.c.n_kv * p.rows_max)), dim3(256), 0, s, a, p);
         BRL_LAUNCH_CHECK("cached_join_kernel");
     }
     if (a.weights) {
         const int chunks = (a.t.max_len + 1023) / 1024;
-        hipLaunchKernelGGL(cached_weights_kernel, dim3((unsigned)(a.t.B * a.c.n_kv * chunks)), dim3(256), 0, s, a, L.p, chunks);
+        hipLaunchKernelGGL(cached_weights_kernel, dim3((unsigned)(a.t.B * a.c.n_kv * chunks)), dim3(256), 0, s, a, p, chunks);
         BRL_LAUNCH_CHECK("cached_weights_kernel");
     }
     return BRL_OK;
 }
 
+template <int DT, int DH>
+int launch_many(const CachedAttention& a, const Layout& L, hipStream_t s) {
+    const Plan& p = L.p;
+    const int units = a.t.B * a.c.n_kv;
+    const dim3 grid((unsigned)(units * p.row_blocks * p.splits)), block(256);
+    if (L.rt == 1) hipLaunchKernelGGL((cached_tiles_kernel<DT, DH, 1>), grid, block, 0, s, a, p);
+    else hipLaunchKernelGGL((cached_tiles_kernel<DT, DH, 2>), grid, block, 0, s, a, p);
+    BRL_LAUNCH_CHECK("cached_tiles_kernel");
+    if (p.splits > 1) {
+        hipLaunchKernelGGL(cached_join_splits_kernel<DH>, dim3((unsigned)(units * p.rows_max)), dim3(64), 0, s, a, p);
+        BRL_LAUNCH_CHECK("cached_join_splits_kernel");
+    }
+    if (a.weights) {
+        const int chunks = (a.t.max_len + 127) / 128;
+        hipLaunchKernelGGL((cached_tile_weights_kernel<DT, DH>), dim3((unsigned)(units * chunks)), block, 0, s, a, p, chunks);
+        BRL_LAUNCH_CHECK("cached_tile_weights_kernel");
+    }
+    return BRL_OK;
+}
+
 template <int DT>
-int launch_stream_dh(const CachedAttention& a, const Layout& L, hipStream_t s) {
+int launch_typed(const CachedAttention& a, const Layout& L, hipStream_t s) {
     switch (a.c.dh) {
-        case 16: return launch_stream<DT, 16>(a, L, s);
-        case 32: return launch_stream<DT, 32>(a, L, s);
-        case 64: return launch_stream<DT, 64>(a, L, s);
-        case 100: return launch_stream<DT, 100>(a, L, s);
-        default: return launch_stream<DT, 128>(a, L, s);
+        case 16: return L.tiles ? launch_many<DT, 16>(a, L, s) : launch_few<DT, 16>(a, L, s);
+        case 32: return L.tiles ? launch_many<DT, 32>(a, L, s) : launch_few<DT, 32>(a, L, s);
+        case 64: return L.tiles ? launch_many<DT, 64>(a, L, s) : launch_few<DT, 64>(a, L, s);
+        case 100: return L.tiles ? launch_many<DT, 100>(a, L, s) : launch_few<DT, 100>(a, L, s);
+        default: return L.tiles ? launch_many<DT, 128>(a, L, s) : launch_few<DT, 128>(a, L, s);
     }
 }
 
@@ -911,19 +1216,17 @@ size_t cached_attention_ws_bytes(const KvView& c, int n_heads, int T, int B, int
 int launch_cached_attention(const CachedAttention& a, void* workspace, hipStream_t s) {
     Layout L = plan_cached(a.c, a.n_heads, a.t.T, a.t.B, a.t.max_new, a.t.max_len, a.weights != nullptr);
     char* base = static_cast<char*>(workspace);
-    LaunchTimer tm(BRL_KC_ATTENTION, s);
-    if (L.p.rows_max > 32) return launch_simple(a, workspace, s);
     Plan& p = L.p;
-    if (p.groups) {
-        p.part_o = reinterpret_cast<float*>(base + L.o_off);
-        p.part_ml = reinterpret_cast<float2*>(base + L.ml_off);
-    }
+    p.part_o = reinterpret_cast<float*>(base + L.o_off);
+    p.part_ml = reinterpret_cast<float2*>(base + L.ml_off);
     if (a.weights) {
         p.lse = reinterpret_cast<float*>(base + L.lse_off);
-        p.scores = reinterpret_cast<float*>(base + L.scores_off);
+        if (L.tiles) p.q = reinterpret_cast<uint4*>(base + L.q_off);
+        else p.scores = reinterpret_cast<float*>(base + L.scores_off);
     }
-    return a.c.dtype == BRL_F32 ? launch_stream_dh<BRL_F32>(a, L, s) : a.c.dtype == BRL_F16 ? launch_stream_dh<BRL_F16>(a, L, s)
-                                                                                           : launch_stream_dh<BRL_I8>(a, L, s);
+    LaunchTimer tm(BRL_KC_ATTENTION, s);
+    return a.c.dtype == BRL_F32 ? launch_typed<BRL_F32>(a, L, s) : a.c.dtype == BRL_F16 ? launch_typed<BRL_F16>(a, L, s)
+                                                                                       : launch_typed<BRL_I8>(a, L, s);
 }
 
 }  // namespace brl

@@ -196,6 +196,13 @@ ATTEND = [
     (64, 12, 4, 32, [40, 0, 90, 12], [0, 8, 17, 0]),              # states without new tokens; groups of three
     (32, 8, 8, 64, [100, 31], [33, 2]),
     (16, 8, 1, 16, [100, 0, 17, 64], [1, 16, 5, 40]),
+    # blocks of all states shared evenly among workgroups, states cut anywhere
+    (64, 4, 2, 32, [1500, 3, 0, 2000, 700, 31], [1, 1, 0, 2, 1, 1]),
+    (128, 5, 1, 64, [2500, 0, 1100], [3, 6, 1]),                  # two row tiles
+    # many rows and long keys: the keys split among workgroups
+    (128, 8, 2, 64, [700], [12]),
+    (100, 3, 3, 32, [900, 40, 0], [70, 2, 0]),
+    (32, 4, 2, 16, [1300], [50]),
 ]
 
 
@@ -233,6 +240,30 @@ def test_attention_over_the_cache_against_the_oracle(dh, hq, hkv, page, cached, 
         assert same_bits(x, c[n]), n
 
 
+@pytest.mark.parametrize("states", [63, 64, 65, 130, 300])
+def test_many_states_of_very_different_length(states):
+    """The shared list of blocks over more states than a wavefront has lanes: most hold little or nothing, a few a great deal."""
+    B, R = _mods()
+    hq, hkv, dh, page = 4, 2, 32, 16
+    rng = np.random.default_rng(states)
+    lens = [int(x) for x in rng.integers(0, 60, states)]
+    for b, n in ((0, 1200), (states - 1, 1700), (states // 2, 1057)):
+        lens[b] = n
+    new = [int(x) for x in rng.integers(0, 3, states)]
+    new[0] = new[-1] = 1
+    lens = [max(a, n) if a % 7 else a for a, n in zip(lens, new)]
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(cu[-1]) + 1
+    cos, sin = tables(1800, dh)
+    c = make_cache(23, hkv, dh, page, lens, np.float16)
+    qkv = synth.normal(23, states, (T, (hq + 2 * hkv) * dh))
+    w = torch.zeros(states, hkv, 1700, device="cuda")
+    got = OnGpu(B, R, c, dh, cos, sin).attend(qkv, hq, cu, 2, lens, weights=w)
+    want, added, reach = K.attend(c, qkv, hq, cu, lens, None, cos, sin)
+    check_rows(got, want, reach, cu, T, states)
+    assert np.all(np.abs(w.cpu().numpy() - added) <= 4e-6 * added)
+
+
 def test_rows_that_see_nothing_are_zeros():
     B, R = _mods()
     hq, hkv, dh, page = 4, 2, 128, 32
@@ -247,14 +278,29 @@ def test_rows_that_see_nothing_are_zeros():
     tree[2, 0] = 1 << 1
     tree[cu[3]:cu[4], 0] = 0b111111          # tokens without a slot are not there to be seen
     clamped = [max(n, 0) for n in lens]
+    c["table"] = np.concatenate([c["table"], np.zeros((5, 128), np.int32)], axis=1)
     for t in (tree, None):
-        w = torch.zeros(5, hkv, 64, device="cuda")
-        got = OnGpu(B, R, c, dh, cos, sin).attend(qkv, hq, cu, max(new), lens, max_len=64, tree=t, weights=w)
         want, added, reach = K.attend(c, qkv, hq, cu, clamped, None, cos, sin, t)
-        check_rows(got, want, reach, cu, T, 5)
         empty = np.all(want == 0, axis=1)
-        assert empty.any() and np.all(got[empty] == 0)
-        assert np.abs(w.cpu().numpy()[:, :, :added.shape[2]] - added).max() <= 4e-6 * max(1.0, added.max())
+        for bound in (64, 4000):                             # short and long bounds on the slots take different forms
+            w = torch.zeros(5, hkv, bound, device="cuda")
+            got = OnGpu(B, R, c, dh, cos, sin).attend(qkv, hq, cu, max(new), lens, max_len=bound, tree=t, weights=w)
+            check_rows(got, want, reach, cu, T, 5)
+            assert empty.any() and np.all(got[empty] == 0)
+            assert np.abs(w.cpu().numpy()[:, :, :added.shape[2]] - added).max() <= 4e-6 * max(1.0, added.max())
+    # the same for few rows
+    few = [1, 1, 2, 2, 1]
+    cu = np.concatenate([[0], np.cumsum(few)]).astype(np.int32)
+    T = int(cu[-1])
+    for t in (np.zeros((T, 1), np.uint32), None):
+        want, added, reach = K.attend(c, qkv[:T], hq, cu, clamped, None, cos, sin, t)
+        for bound in (64, 4000):
+            w = torch.zeros(5, hkv, bound, device="cuda")
+            got = OnGpu(B, R, c, dh, cos, sin).attend(qkv[:T], hq, cu, 2, lens, max_len=bound, tree=t, weights=w)
+            check_rows(got, want, reach, cu, T, 5)
+            empty = np.all(want == 0, axis=1)
+            assert empty.any() and np.all(got[empty] == 0)
+            assert np.abs(w.cpu().numpy()[:, :, :added.shape[2]] - added).max() <= 4e-6 * max(1.0, added.max())
 
 
 def test_mask_words_short_of_the_new_tokens():
