@@ -139,7 +139,7 @@ int append_typed(AppendArgs a, hipStream_t s) {
 // One workgroup per list.  The threshold (the key of the last slot that is taken) is found bit group by bit group: a histogram
 // of the next bits of the keys that agree with the threshold so far, scanned from the top.  Then one pass in slot order takes
 // what lies above it and the first of those equal to it.
-constexpr int SEL_THREADS = 1024, SEL_BINS = 2048;
+constexpr int SEL_THREADS = 1024, SEL_BINS = 2048, SEL_COPIES = 8;
 
 struct SelectArgs {
     const float* weights;
@@ -156,32 +156,47 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// sum over the workgroup of what lies in front of this thread, and the total
-__device__ __forceinline__ uint32_t scan_before(uint32_t v, uint32_t* waves, uint32_t& total) {
+// inclusive sum over a wavefront: rows of 16 lanes, then across them (data-parallel primitives, no trip through LDS)
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);       // from 1, 2, 4, 8 lanes below, inside a row
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);       // row 0's sum to row 1, row 2's to row 3
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);       // lane 31's to rows 2 and 3
+    return v;
+}
+// sums over the workgroup of what lies in front of this thread, for two numbers, and the totals
+struct Before {
+    uint32_t a, b, all_a, all_b;
+};
+__device__ __forceinline__ Before scan_before(uint32_t a, uint32_t b, uint2* waves) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t x = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t y = __shfl_up(x, d, 64);
-        if (lane >= d) x += y;
-    }
-    if (lane == 63) waves[wave] = x;
+    const uint32_t x = wave_scan(a), y = wave_scan(b);
+    if (lane == 63) waves[wave] = make_uint2(x, y);
     __syncthreads();
-    uint32_t before = 0, sum = 0;
-#pragma unroll
-    for (int w = 0; w < SEL_THREADS / 64; ++w) {
-        if (w < wave) before += waves[w];
-        sum += waves[w];
-    }
-    total = sum;
+    // every wavefront scans the wavefronts' totals itself
+    const uint2 t = waves[lane % (SEL_THREADS / 64)];
+    const uint32_t p = wave_scan(lane < SEL_THREADS / 64 ? t.x : 0u), q = wave_scan(lane < SEL_THREADS / 64 ? t.y : 0u);
+    Before r;
+    r.all_a = lane_value(p, SEL_THREADS / 64 - 1);
+    r.all_b = lane_value(q, SEL_THREADS / 64 - 1);
+    r.a = x - a + (wave ? lane_value(p, wave - 1) : 0u);
+    r.b = y - b + (wave ? lane_value(q, wave - 1) : 0u);
     __syncthreads();
-    return before + x - v;
+    return r;
 }
 
+// HELD: quads of weights that a thread keeps in registers (4 HELD neighbouring slots, all of a list in 4096 HELD slots); 0: the list
+// is read again for each pass, 4096 slots at a time.  8000 slots, 320 lists: 20.4 us when every list was read four times.
+template <int HELD>
 __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a) {
-    __shared__ uint32_t hist[SEL_BINS];
-    __shared__ uint32_t waves[SEL_THREADS / 64];
+    // Weights crowd into few bins of the first pass (their exponents): eight copies of each bin, side by side in neighbouring
+    // banks, so that a wavefront's lanes do not queue for one address.
+    __shared__ __attribute__((aligned(16))) uint32_t hist[SEL_BINS * SEL_COPIES];
+    __shared__ uint2 waves[SEL_THREADS / 64];
     __shared__ uint32_t s_bin, s_above;
+    constexpr int Q = HELD ? HELD : 1;
     const int b = blockIdx.x / a.n_kv, tid = threadIdx.x;
     const int len = clampi(a.lens[b], 0, a.max_len);
     int32_t* kept = a.kept + (size_t)blockIdx.x * a.keep;
@@ -192,102 +207,167 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
     }
     const int mid = a.keep - a.first - a.recent;      // to be taken out of slots first .. len - recent - 1, more than mid of them
     const int lo = a.first, hi = len - a.recent;
+    const float* w = a.weights + (size_t)blockIdx.x * a.ld;
+    uint32_t key[4 * Q];                              // 0 (below every key of a weight) outside lo .. hi - 1
+    auto read = [&](int i0) {
+        float x[4 * Q];
+        const bool whole = ((a.ld | (size_t)(reinterpret_cast<uintptr_t>(a.weights) >> 2)) & 3) == 0;
+#pragma unroll
+        for (int j = 0; j < Q; ++j) {
+            const int i = i0 + 4 * j;
+            if (whole && i + 4 <= hi) {
+                *reinterpret_cast<float4*>(x + 4 * j) = *reinterpret_cast<const float4*>(w + i);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[4 * j + e] = i + e < hi ? w[i + e] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4 * Q; ++e) key[e] = i0 + e >= lo && i0 + e < hi ? weight_key(x[e]) : 0u;
+    };
+    const int steps = HELD ? 1 : (hi + 4 * SEL_THREADS - 1) / (4 * SEL_THREADS);
+    if (HELD) read(tid * 4 * Q);
     for (int i = tid; i < a.first; i += SEL_THREADS) kept[i] = i;
     for (int i = tid; i < a.recent; i += SEL_THREADS) kept[a.first + mid + i] = hi + i;
     if (mid == 0) return;
-    const float* w = a.weights + (size_t)blockIdx.x * a.ld;
     uint32_t prefix = 0, want = mid;                  // still to be taken among the keys that begin with prefix
     int shift = 32;
     for (int pass = 0; pass < 3; ++pass) {
         const int bits = pass < 2 ? 11 : 10, above = shift;
         shift -= bits;
-        for (int i = tid; i < SEL_BINS; i += SEL_THREADS) hist[i] = 0;
+        for (int i = tid; i < SEL_BINS * SEL_COPIES / 4; i += SEL_THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        for (int i = lo + tid; i < hi; i += SEL_THREADS) {
-            const uint32_t k = weight_key(w[i]);
-            if (above == 32 || (k >> above) == prefix) atomicAdd(&hist[(k >> shift) & ((1u << bits) - 1)], 1u);
+        for (int step = 0; step < steps; ++step) {
+            if (!HELD) read((step * SEL_THREADS + tid) * 4);
+#pragma unroll
+            for (int e = 0; e < 4 * Q; ++e)
+                if (key[e] && (pass == 0 || key[e] >> above == prefix)) atomicAdd(&hist[((key[e] >> shift) & ((1u << bits) - 1)) * SEL_COPIES + tid % SEL_COPIES], 1u);
         }
         __syncthreads();
         // bins from the top: thread t has bins top - 2 t and top - 2 t - 1
         const int top = (1 << bits) - 1, b0 = top - 2 * tid, b1 = b0 - 1;
-        const uint32_t h0 = b0 >= 0 ? hist[b0] : 0, h1 = b1 >= 0 ? hist[b1] : 0;
-        uint32_t total;
-        const uint32_t before = scan_before(h0 + h1, waves, total);
+        auto in_bin = [&](int i) {
+            if (i < 0) return 0u;
+            const uint4 x = reinterpret_cast<const uint4*>(hist)[2 * i], y = reinterpret_cast<const uint4*>(hist)[2 * i + 1];
+            return x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+        };
+        const uint32_t h0 = in_bin(b0), h1 = in_bin(b1);
+        const uint32_t before = scan_before(h0 + h1, 0u, waves).a;
         if (before < want && want <= before + h0) { s_bin = b0; s_above = before; }
         else if (before + h0 < want && want <= before + h0 + h1) { s_bin = b1; s_above = before + h0; }
         __syncthreads();
         prefix = (prefix << bits) | s_bin;
         want -= s_above;
-        __syncthreads();
     }
     // in slot order: all above the threshold, the first `want` equal to it
-    uint32_t greater = 0, equal = 0;                  // so far
-    for (int i0 = lo; i0 < hi; i0 += SEL_THREADS) {
-        const int i = i0 + tid;
-        const uint32_t k = i < hi ? weight_key(w[i]) : 0;
-        const bool g = i < hi && k > prefix, e = i < hi && k == prefix;
-        uint32_t total;
-        const uint32_t before = scan_before((g ? 1u : 0u) | (e ? 0x10000u : 0u), waves, total);
-        const uint32_t eb = equal + (before >> 16), gb = greater + (before & 0xffffu);
-        if (g || (e && eb < want)) kept[a.first + gb + (eb < want ? eb : want)] = i;
-        greater += total & 0xffffu;
-        equal += total >> 16;
+    uint32_t greater = 0, equal = 0;                  // in front of the step
+    for (int step = 0; step < steps; ++step) {
+        const int i0 = HELD ? tid * 4 * Q : (step * SEL_THREADS + tid) * 4;
+        if (!HELD) read(i0);
+        uint32_t g = 0, q = 0;
+#pragma unroll
+        for (int e = 0; e < 4 * Q; ++e) {
+            g += key[e] > prefix;
+            q += key[e] == prefix;
+        }
+        const Before s = scan_before(g, q, waves);
+        uint32_t gb = greater + s.a, qb = equal + s.b;
+#pragma unroll
+        for (int e = 0; e < 4 * Q; ++e) {
+            const bool over = key[e] > prefix, same = key[e] == prefix;
+            if (over || (same && qb < want)) kept[a.first + gb + (qb < want ? qb : want)] = i0 + e;
+            gb += over;
+            qb += same;
+        }
+        greater += s.all_a;
+        equal += s.all_b;
     }
 }
 
 // ---- compact ----
 // Rows move to lower slots of the same pages (kept[i] >= start + i).  One workgroup owns one column slice of the rows of one
 // head and walks them in ascending order, a chunk at a time: what a chunk overwrites lies below the sources of every later
-// chunk, so the only order needed is that all of a chunk has been read before any of it is written.
+// chunk, so the only order needed is that all of a chunk has been read before any of it is written.  While a chunk's rows are
+// on their way the places of the next chunk's are looked up (list, then page table).
 constexpr int CP_THREADS = 256, CP_ITEMS = 8, CP_INFLIGHT = CP_THREADS * CP_ITEMS;
 
+typedef uint32_t chunk16 __attribute__((ext_vector_type(4)));
+
+struct Move {
+    const CompactArgs& a;
+    const int32_t* kept;
+    int b, h, len, start, count;
+    bool paged;
+    // row indices of entry r's source and target, from = -1: nothing moves
+    __device__ __forceinline__ int2 place(int r) const {
+        if (r >= count) return make_int2(-1, -1);
+        const int src = kept[r], dst = start + r;
+        if (src <= dst || src >= len) return make_int2(-1, -1);
+        if (!paged) return make_int2(src, dst);
+        const int from = kv_row_index(a.c, b, h, src), at = kv_row_index(a.c, b, h, dst);
+        return at < 0 ? make_int2(-1, -1) : make_int2(from, at);
+    }
+};
+
+// units `first` .. first + units - 1 of every row, rows of `row_units` units of type T
 template <class T>
-__device__ __forceinline__ void move_rows(const CompactArgs& a, T* pool, size_t row_units, int first_unit, int units, int b, int h, int len,
-                                          int start, int count, bool paged) {
-    const int32_t* kept = a.kept + ((size_t)b * a.kept_heads + (a.kept_heads == 1 ? 0 : h)) * a.ld_kept;
+__device__ __forceinline__ void move_rows(const Move& m, T* pool, int row_units, int first, int units, int2* places) {
     const int rows = CP_INFLIGHT / units;             // of a chunk
-    for (int r0 = 0; r0 < count; r0 += rows) {
+    const int tid = threadIdx.x, q = CP_THREADS / units, rem = CP_THREADS % units;
+    for (int i = tid; i < rows; i += CP_THREADS) places[i] = m.place(i);
+    __syncthreads();
+    int buf = 0;
+    for (int r0 = 0; r0 < m.count; r0 += rows) {
         T v[CP_ITEMS];
-        long long to[CP_ITEMS];
+        size_t to[CP_ITEMS];
+        bool moves[CP_ITEMS];
+        int r = tid / units, u = tid % units;
 #pragma unroll
         for (int e = 0; e < CP_ITEMS; ++e) {
-            const int item = e * CP_THREADS + threadIdx.x, r = r0 + item / units, u = first_unit + item % units;
-            to[e] = -1;
-            if (item >= rows * units || r >= count) continue;
-            const int src = kept[r], dst = start + r;
-            if (src <= dst || src >= len) continue;
-            const int from = paged ? kv_row_index(a.c, b, h, src) : src;
-            const int at = paged ? kv_row_index(a.c, b, h, dst) : dst;
-            if (from < 0 || at < 0) continue;
-            v[e] = pool[(size_t)from * row_units + u];
-            to[e] = (long long)at * (long long)row_units + u;
+            // (what does not move reads row 0: loads that might not happen would each be waited for)
+            const int2 x = r < rows ? places[buf * CP_INFLIGHT + r] : make_int2(-1, -1);
+            moves[e] = x.x >= 0;
+            v[e] = pool[(size_t)(moves[e] ? x.x : 0) * row_units + first + u];
+            to[e] = (size_t)(moves[e] ? x.y : 0) * row_units + first + u;
+            r += q;
+            u += rem;
+            if (u >= units) {
+                u -= units;
+                ++r;
+            }
         }
+        buf ^= 1;
+        if (r0 + rows < m.count)
+            for (int i = tid; i < rows; i += CP_THREADS) places[buf * CP_INFLIGHT + i] = m.place(r0 + rows + i);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // read, not only requested
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < CP_ITEMS; ++e)
-            if (to[e] >= 0) pool[to[e]] = v[e];
+            if (moves[e]) pool[to[e]] = v[e];
     }
+    __syncthreads();
 }
 
 __global__ __launch_bounds__(CP_THREADS) void cache_compact_kernel(CompactArgs a, int slices, int units, int row_units) {
+    __shared__ int2 places[2 * CP_INFLIGHT];
     const int parts = 2 * slices + 1;
     const int part = blockIdx.x % parts, h = blockIdx.x / parts % a.c.n_kv, b = blockIdx.x / (parts * a.c.n_kv);
     const int len = clampi(a.lens[b], 0, a.max_len);
     const int start = a.start ? clampi(a.start[b], 0, len) : 0;
     const int most = len - start < a.ld_kept ? len - start : a.ld_kept;
-    const int count = clampi(a.counts[b], 0, most);
+    Move m = {a, a.kept + ((size_t)b * a.kept_heads + (a.kept_heads == 1 ? 0 : h)) * a.ld_kept, b, h, len, start, clampi(a.counts[b], 0, most), true};
     if (part < 2 * slices) {
         const int first = part % slices * units;
-        const int n = row_units - first < units ? row_units - first : units;
-        move_rows(a, reinterpret_cast<uint4*>(part < slices ? a.c.k : a.c.v), (size_t)row_units, first, n, b, h, len, start, count, true);
+        move_rows(m, reinterpret_cast<chunk16*>(part < slices ? a.c.k : a.c.v), row_units, first,
+                  row_units - first < units ? row_units - first : units, places);
         return;
     }
     if (a.c.dtype == BRL_I8) {
-        move_rows(a, a.c.ks, 1, 0, 1, b, h, len, start, count, true);
-        move_rows(a, a.c.vs, 1, 0, 1, b, h, len, start, count, true);
+        move_rows(m, a.c.ks, 1, 0, 1, places);
+        move_rows(m, a.c.vs, 1, 0, 1, places);
     }
-    if (a.weights) move_rows(a, a.weights + ((size_t)b * a.c.n_kv + h) * a.ld_weights, 1, 0, 1, b, h, len, start, count, false);
+    m.paged = false;
+    if (a.weights) move_rows(m, a.weights + ((size_t)b * a.c.n_kv + h) * a.ld_weights, 1, 0, 1, places);
 }
 
 }  // namespace
@@ -305,14 +385,23 @@ int launch_cache_select(const float* weights, size_t ld_weights, int B, int n_kv
     a.weights = weights; a.ld = ld_weights; a.lens = lens; a.n_kv = n_kv; a.max_len = max_len; a.keep = keep;
     a.first = first; a.recent = recent; a.kept = kept; a.counts = counts;
     LaunchTimer tm(BRL_KC_ATTENTION, s);
-    hipLaunchKernelGGL(cache_select_kernel, dim3((unsigned)(B * n_kv)), dim3(SEL_THREADS), 0, s, a);
+    const dim3 grid((unsigned)(B * n_kv)), block(SEL_THREADS);
+    if (max_len <= 1 * 4 * SEL_THREADS) hipLaunchKernelGGL(cache_select_kernel<1>, grid, block, 0, s, a);
+    else if (max_len <= 2 * 4 * SEL_THREADS) hipLaunchKernelGGL(cache_select_kernel<2>, grid, block, 0, s, a);
+    else if (max_len <= 4 * 4 * SEL_THREADS) hipLaunchKernelGGL(cache_select_kernel<4>, grid, block, 0, s, a);
+    else if (max_len <= 16 * 4 * SEL_THREADS) hipLaunchKernelGGL(cache_select_kernel<16>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(cache_select_kernel<0>, grid, block, 0, s, a);
     BRL_LAUNCH_CHECK("cache_select_kernel");
     return BRL_OK;
 }
 
 int launch_cache_compact(const CompactArgs& a, hipStream_t s) {
     const int row_units = a.c.row * kv_bytes(a.c.dtype) / 16;
-    const int units = row_units < 4 ? row_units : 4, slices = (row_units + units - 1) / units;
+    // Whole rows where the heads alone fill the chip; narrower slices, down to 32 bytes, where there are few of them.
+    int slices = 1;
+    while ((long long)a.B * a.c.n_kv * 2 * slices < 512 && row_units / (2 * slices) >= 2) slices *= 2;
+    const int units = (row_units + slices - 1) / slices;
+    slices = (row_units + units - 1) / units;
     LaunchTimer tm(BRL_KC_ATTENTION, s);
     hipLaunchKernelGGL(cache_compact_kernel, dim3((unsigned)(a.B * a.c.n_kv * (2 * slices + 1))), dim3(CP_THREADS), 0, s, a, slices, units,
                        row_units);
