@@ -141,10 +141,12 @@ struct ValueLoads {
         constexpr int HALF = 16 * S::CPR;                              // chunks of 16 rows
 #pragma unroll
         for (int i = 0; i < S::NV; ++i) {
-            const int idx = i * 64 + lane;
-            if (S::NV * 64 > 32 * S::CPR && idx >= 32 * S::CPR) continue;
+            int idx = i * 64 + lane;
+            // past the end: the last chunk again, not stored (a load that might not happen is waited for before its registers'
+            // next use, which is the load of the next block)
+            if (S::NV * 64 > 32 * S::CPR && idx >= 32 * S::CPR) idx = 32 * S::CPR - 1;
             if ((i + 1) * 64 <= HALF) raw[i] = reinterpret_cast<const uint4*>(lo + i * 1024)[(unsigned)lane];
-            else if (i * 64 >= HALF) raw[i] = reinterpret_cast<const uint4*>(hi + (i * 64 - HALF) * 16)[(unsigned)lane];
+            else if (i * 64 >= HALF) raw[i] = reinterpret_cast<const uint4*>(hi)[(unsigned)(idx - HALF)];
             else raw[i] = idx >= HALF ? reinterpret_cast<const uint4*>(hi)[(unsigned)(idx - HALF)] : reinterpret_cast<const uint4*>(lo)[(unsigned)idx];
         }
     }
@@ -209,16 +211,22 @@ struct ValueReads {
     }
 };
 
+struct QueryRow {
+    const float *x, *ct, *sn;          // a query row, the cosines and sines of its position
+    __device__ __forceinline__ QueryRow(const CachedAttention& a, const StateTokens& st, int h, int group, int r) {
+        const int i = r / group, row = st.row0 + i, pos = rope_position(a.t, row, st.base + i), dh = a.c.dh;
+        x = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * dh) + (h * group + r % group) * dh;
+        ct = a.t.cos_t + (size_t)pos * (dh / 2);
+        sn = a.t.sin_t + (size_t)pos * (dh / 2);
+    }
+};
 // Eight components d0 .. of a query row, rotated, scaled and split into an operand's hi and lo words.  Fragments hold, in lane
 // 16 g + c, components 32 s + 8 g .. of row c.
 template <class S>
 struct QueryPart {
     float x[8], y[8], c[8], w[8];      // components, their partners, cosines, sines
-    __device__ __forceinline__ void request(const CachedAttention& a, const StateTokens& st, int h, int group, int r, int d0) {
+    __device__ __forceinline__ void request(const float* q, const float* ct, const float* sn, int d0) {
         constexpr int DH = S::DH, half = DH / 2;
-        const int i = r / group, row = st.row0 + i, pos = rope_position(a.t, row, st.base + i);
-        const float* q = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * DH) + (h * group + r % group) * DH;
-        const float *ct = a.t.cos_t + (size_t)pos * half, *sn = a.t.sin_t + (size_t)pos * half;
         if constexpr (DH % 16 == 0) {                                  // eight components lie in one half
             const int d = d0 < DH ? d0 : 0, f = d < half ? d : d - half, partner = d < half ? d + half : d - half;
 #pragma unroll
@@ -228,11 +236,15 @@ struct QueryPart {
                 *reinterpret_cast<float4*>(c + e) = *reinterpret_cast<const float4*>(ct + f + e);
                 *reinterpret_cast<float4*>(w + e) = *reinterpret_cast<const float4*>(sn + f + e);
             }
-        } else {
+        } else {                                                       // two do
+            static_assert(DH % 4 == 0, "pairs do not straddle the halves");
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 8; e += 2) {
                 const int d = d0 + e < DH ? d0 + e : 0, f = d < half ? d : d - half, partner = d < half ? d + half : d - half;
-                x[e] = q[d]; y[e] = q[partner]; c[e] = ct[f]; w[e] = sn[f];
+                *reinterpret_cast<float2*>(x + e) = *reinterpret_cast<const float2*>(q + d);
+                *reinterpret_cast<float2*>(y + e) = *reinterpret_cast<const float2*>(q + partner);
+                *reinterpret_cast<float2*>(c + e) = *reinterpret_cast<const float2*>(ct + f);
+                *reinterpret_cast<float2*>(w + e) = *reinterpret_cast<const float2*>(sn + f);
             }
         }
     }
@@ -257,7 +269,8 @@ struct QueryJob {
     QueryPart<S> part;
     __device__ __forceinline__ void request(const CachedAttention& a, const StateTokens& st, int h, int group, int rows, int job) {
         const int lane = job & 63, r = (job >> 6) / S::KS * 16 + (lane & 15);
-        part.request(a, st, h, group, r < rows ? r : rows - 1, 32 * ((job >> 6) % S::KS) + 8 * (lane >> 4));
+        const QueryRow q(a, st, h, group, r < rows ? r : rows - 1);
+        part.request(q.x, q.ct, q.sn, 32 * ((job >> 6) % S::KS) + 8 * (lane >> 4));
     }
     __device__ __forceinline__ void store(uint4* lds, int rows, int job) const {
         const int lane = job & 63, s = (job >> 6) % S::KS, rt = (job >> 6) / S::KS;
@@ -750,8 +763,8 @@ struct SharedLoads {
         constexpr int HALF = 16 * S::CPR;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int idx = i * 256 + tid;
-            if (N * 256 > 32 * S::CPR && idx >= 32 * S::CPR) continue;
+            int idx = i * 256 + tid;                                   // (past the end: the last chunk again, see ValueLoads)
+            if (N * 256 > 32 * S::CPR && idx >= 32 * S::CPR) idx = 32 * S::CPR - 1;
             const size_t at = idx >= HALF ? hi_at + (size_t)((idx - HALF) * 16) : lo_at + (size_t)(idx * 16);
             k[i] = *reinterpret_cast<const uint4*>(c.k + at);
             v[i] = *reinterpret_cast<const uint4*>(c.v + at);
@@ -842,14 +855,18 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
         if (hi < 0) x &= 0x0000ffffu;
         return x;
     };
-    SharedLoads<S> load;
-    int lo = -1, hi = -1;
-    if (first < last) {
-        pages(first);
-        lo = lane_value(page_lo, 0);
-        hi = lane_value(page_hi, 0);
-        load.request(a.c, lo, hi, tid);
-    }
+    // Blocks under way in registers.  One row tile per wavefront is less work on a block than the way from memory takes: two.
+    constexpr int DEPTH = RT == 1 ? 2 : 1;
+    SharedLoads<S> load[DEPTH];
+    int lo[DEPTH + 1], hi[DEPTH + 1];                                  // of the block worked on and of those under way
+    int ahead = 0;
+    if (first < last) pages(first);
+    auto locate = [&](int t, int i) {
+        lo[i] = t < last ? lane_value(page_lo, ahead) : -1;
+        hi[i] = t < last ? lane_value(page_hi, ahead) : -1;
+    };
+    locate(first, 0);
+    load[0].request(a.c, lo[0], hi[0], tid);
     // this wavefront's rows
     const int w0 = r0 + wave * 16 * RT, w1 = w0 + 16 * RT - 1 < r1 ? w0 + 16 * RT - 1 : r1;
     const bool busy = w0 <= r1;
@@ -863,10 +880,11 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
         row[r].clear();
         const int rr = w0 + r * 16 + c;
         token[r] = (rr < rows ? rr : rows - 1) / p.group;
+        const QueryRow from(a, st, h, p.group, rr < rows ? rr : rows - 1);
 #pragma unroll
         for (int s = 0; s < S::KS; ++s) {
             QueryPart<S> q;
-            q.request(a, st, h, p.group, rr < rows ? rr : rows - 1, 32 * s + 8 * g);
+            q.request(from.x, from.ct, from.sn, 32 * s + 8 * g);
             uint4 x, y;
             q.split(rr < rows, 32 * s + 8 * g, x, y);
             qh[r][s] = __builtin_bit_cast(v8h, x);
@@ -885,17 +903,26 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
         }
     }
     float unit_scale = 0x1p126f;                                       // int8: power of two that the sums are multiplied by
-    if (first < last) load.store(s_kv[0], s_scale[0], tid, there_of(first, lo, hi));
+    load[0].store(s_kv[0], s_scale[0], tid, there_of(first, lo[0], hi[0]));
+    if constexpr (DEPTH == 2) {
+        ++ahead;
+        locate(first + 1, 1);
+        load[1].request(a.c, lo[1], hi[1], tid);
+    }
     __syncthreads();
-    int ahead = 0, buf = 0;
-    for (int t = first; t < last; ++t) {
+    int buf = 0;
+    for (int t0 = first; t0 < last; t0 += DEPTH) {
+#pragma unroll
+    for (int turn = 0; turn < DEPTH; ++turn) {
+        const int t = t0 + turn;
+        if (DEPTH > 1 && t >= last) break;
         if (++ahead == 64) {
             ahead = 0;
-            pages(t + 1);
+            pages(t + DEPTH);
         }
-        const bool more = t + 1 < last;
-        const int next_lo = more ? lane_value(page_lo, ahead) : -1, next_hi = more ? lane_value(page_hi, ahead) : -1;
-        load.request(a.c, next_lo, next_hi, tid);
+        // (block t was in load[turn])
+        locate(t + DEPTH, DEPTH);
+        load[turn].request(a.c, lo[DEPTH], hi[DEPTH], tid);
         __builtin_amdgcn_sched_barrier(0);
         if (t < wave_blocks) {
             const char* keys = s_kv[buf];
@@ -937,8 +964,8 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[r][e] *= kf[e];
             }
-            if (t * 32 + 32 > all_see || lo < 0 || hi < 0) {
-                const uint32_t mine = there_of(t, lo, hi) >> (8 * g) & 0xffu;
+            if (t * 32 + 32 > all_see || lo[0] < 0 || hi[0] < 0) {
+                const uint32_t mine = there_of(t, lo[0], hi[0]) >> (8 * g) & 0xffu;
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     const uint32_t bits = mine & visible_bits(a, st, token[r], t * 32 + 8 * g);
@@ -967,11 +994,15 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
             block_values<S, RT>(vals, s, row, lane);
         }
         __builtin_amdgcn_sched_barrier(0);
-        load.store(s_kv[buf ^ 1], s_scale[buf ^ 1], tid, more ? there_of(t + 1, next_lo, next_hi) : 0u);
-        lo = next_lo;
-        hi = next_hi;
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+            lo[i] = lo[i + 1];
+            hi[i] = hi[i + 1];
+        }
+        load[(turn + 1) % DEPTH].store(s_kv[buf ^ 1], s_scale[buf ^ 1], tid, there_of(t + 1, lo[0], hi[0]));
         buf ^= 1;
         __syncthreads();
+    }
     }
     if (!busy) return;
 #pragma unroll
@@ -1128,10 +1159,14 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
         L.rt = p.rows_max <= 64 ? 1 : 2;
         p.row_blocks = (p.rows_max + 64 * L.rt - 1) / (64 * L.rt);
         p.rows_pad = p.row_blocks * 64 * L.rt;
+        // 512 workgroups run at a time.  A workgroup costs its blocks and about four more (queries, first loads, end), parts that
+        // have to be joined another four; the split with the shortest sum of rounds.
         const long long groups = (long long)units * p.row_blocks;
-        long long s = (1024 + groups - 1) / groups;
-        if (s > blocks / 8) s = blocks / 8;
-        p.splits = s < 1 ? 1 : (int)s;
+        long long best = 0;
+        for (int s = 1; s <= 16 && (s == 1 || blocks / s >= 8); ++s) {
+            const long long cost = (groups * s + 511) / 512 * ((blocks + s - 1) / s + 4) + (s > 1 ? 4 : 0);
+            if (s == 1 || cost < best) { best = cost; p.splits = s; }
+        }
         parts = p.splits > 1 ? (size_t)units * p.rows_pad * p.splits : 0;
     }
     const size_t rows = (size_t)units * p.rows_pad;
