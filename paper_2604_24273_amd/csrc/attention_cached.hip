@@ -7,9 +7,9 @@
 // products with one such operand take two matrix instructions, with two three (lo * lo is dropped).  int8 codes are exact
 // in fp16; a key's scale multiplies its scores, a value's scale its probabilities.
 //
-// Order of the keys.  A block of 32 keys is two key tiles; row 4 a + r of tile t is key 8 a + 4 t + r.  Lane l = 16 g + c of
-// S^T then holds row c's scores of the keys 8 g .. 8 g + 7, and those are the eight contraction slots that lane has to
-// fill as operand P of the second product: the probabilities never leave their lane.
+// Order of the keys.  A block of 32 keys is two key tiles of 16.  Lane l = 16 g + c of S^T holds row c's scores of the keys 4 g ..
+// 4 g + 3 of both tiles.  The contraction of the second product may run over the keys in any order: with those eight as the
+// slots that lane has to fill of operand P, the probabilities never leave their lane.
 #include <cstring>
 
 #include "common.hpp"
@@ -68,12 +68,8 @@ struct Shape {
 // x 16 bytes of a key fragment and the 16 rows x 32 bytes of a transposing read fall on all banks.
 template <class S>
 __device__ __forceinline__ int lds_chunk(int key, int c) {
-    int f;
-    if constexpr (S::NCH == 16) f = (key & 3) | ((key >> 1) & 12);
-    else if constexpr (S::NCH == 8) f = ((key >> 1) & 1) | ((key >> 2) & 6);
-    else if constexpr (S::NCH == 4) f = (key >> 3) & 3;
-    else f = (key >> 3) & 1;
-    return key * S::LS + ((c ^ f) << 4);
+    constexpr int SKIP = S::NCH == 16 ? 0 : S::NCH == 8 ? 1 : S::NCH == 4 ? 2 : 3;   // rows that lie side by side in 256 bytes
+    return key * S::LS + ((c ^ ((key & 15) >> SKIP)) << 4);
 }
 
 // A block of 32 slots lies in two halves of 16 (pages hold 16 at least): lo and hi are their first rows in the pool, -1 where
@@ -90,17 +86,20 @@ struct KeyLoads {
     typename Raw<S::DT>::type raw[2][S::KS][S::KL];
     __device__ __forceinline__ void request(const char* pool, int lo, int hi, int lane) {
         const int c = lane & 15, g = lane >> 4;
-        const char *pl = pool + (size_t)(lo < 0 ? 0 : lo) * S::RB, *ph = pool + (size_t)(hi < 0 ? 0 : hi) * S::RB;
-        const char* p = ((c >> 3) ? ph : pl) + (unsigned)((((c >> 2) & 1) * 8 + (c & 3)) * S::RB + 8 * g * S::SZ);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
+            const int row = t ? hi : lo;
+            const char* p = pool + (size_t)(row < 0 ? 0 : row) * S::RB;          // (the same for all lanes)
 #pragma unroll
             for (int s = 0; s < S::KS; ++s) {
-                const char* q = p + t * 4 * S::RB + s * 32 * S::SZ;
-                if (S::KS * 32 > S::ROW && s == S::KS - 1 && 32 * s + 8 * g + 8 > S::ROW) q = p;      // (a row ends inside the step)
+                unsigned at = (unsigned)(c * S::RB + 8 * g * S::SZ);
+                if (S::KS * 32 > S::ROW && s == S::KS - 1 && 32 * s + 8 * g + 8 > S::ROW) at = (unsigned)(c * S::RB);   // (a row ends inside the step)
+                else at += (unsigned)(s * 32 * S::SZ);
 #pragma unroll
-                for (int i = 0; i < S::KL; ++i) raw[t][s][i] = reinterpret_cast<const typename Raw<S::DT>::type*>(q)[i];
+                for (int i = 0; i < S::KL; ++i)
+                    raw[t][s][i] = *reinterpret_cast<const typename Raw<S::DT>::type*>(p + (at + (unsigned)(i * 16)));
             }
+        }
     }
     __device__ __forceinline__ void fragment(int t, int s, int lane, v8h (&f)[S::PL]) const {
         uint32_t w[S::PL][4];
@@ -145,9 +144,9 @@ struct ValueLoads {
             // past the end: the last chunk again, not stored (a load that might not happen is waited for before its registers'
             // next use, which is the load of the next block)
             if (S::NV * 64 > 32 * S::CPR && idx >= 32 * S::CPR) idx = 32 * S::CPR - 1;
-            if ((i + 1) * 64 <= HALF) raw[i] = reinterpret_cast<const uint4*>(lo + i * 1024)[(unsigned)lane];
-            else if (i * 64 >= HALF) raw[i] = reinterpret_cast<const uint4*>(hi)[(unsigned)(idx - HALF)];
-            else raw[i] = idx >= HALF ? reinterpret_cast<const uint4*>(hi)[(unsigned)(idx - HALF)] : reinterpret_cast<const uint4*>(lo)[(unsigned)idx];
+            if ((i + 1) * 64 <= HALF) raw[i] = *reinterpret_cast<const uint4*>(lo + (unsigned)(idx * 16));
+            else if (i * 64 >= HALF) raw[i] = *reinterpret_cast<const uint4*>(hi + (unsigned)((idx - HALF) * 16));
+            else raw[i] = *reinterpret_cast<const uint4*>(idx >= HALF ? hi + (unsigned)((idx - HALF) * 16) : lo + (unsigned)(idx * 16));
         }
     }
     __device__ __forceinline__ void store(char* lds, int lane) const {
@@ -185,15 +184,15 @@ __device__ __forceinline__ void clear_rows(char* lds, int lane, uint32_t there) 
         if (!(there >> (i / S::NCH % 32) & 1u)) reinterpret_cast<uint4*>(lds)[i] = make_uint4(0, 0, 0, 0);
 }
 
-// Transposed value fragment: of components 16 d + (lane & 15) the keys 8 g .. 8 g + 7.  A transposing read gives each lane
-// of 16 one column of 4 rows x 16 halfs whose row i the lanes 4 i .. 4 i + 3 address.  (Keys four apart have their chunks
-// permuted alike, so the second read is the first one's address and a constant.)
+// Transposed value fragment: of components 16 d + (lane & 15) the keys 4 g .. 4 g + 3 of both tiles.  A transposing read gives
+// each lane of 16 one column of 4 rows x 16 halfs whose row i the lanes 4 i .. 4 i + 3 address.  (Keys sixteen apart have their
+// chunks permuted alike, so the second read is the first one's address and a constant.)
 template <class S>
 struct ValueReads {
     const char* base;
     int x;
     __device__ __forceinline__ ValueReads(const char* lds, int lane) {
-        const int c = lane & 15, key = 8 * (lane >> 4) + (c >> 2);
+        const int c = lane & 15, key = 4 * (lane >> 4) + (c >> 2);
         const int at = lds_chunk<S>(key, (c & 3) >> 1);
         base = lds + key * S::LS + (c & 1) * 8;
         x = at - key * S::LS;
@@ -204,7 +203,7 @@ struct ValueReads {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             typedef __attribute__((address_space(3))) v4fp* lds_ptr;
-            const v4fp v = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_ptr)(p + plane * S::PLANE + u * 4 * S::LS));
+            const v4fp v = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_ptr)(p + plane * S::PLANE + u * 16 * S::LS));
             r[u] = __builtin_bit_cast(uint2, v);
         }
         return __builtin_bit_cast(v8h, make_uint4(r[0].x, r[0].y, r[1].x, r[1].y));
@@ -281,18 +280,22 @@ struct QueryJob {
     }
 };
 
-// which of the slots slot0 .. slot0 + 7 token i sees, for blocks that not every row sees whole
+// which of the slots slot0 .. slot0 + 31 token i sees, for blocks that not every row sees whole
 __device__ __forceinline__ uint32_t visible_bits(const CachedAttention& a, const StateTokens& st, int i, int slot0) {
     if (!a.tree) {
         const int n = st.base + i + 1 - slot0;                         // from slot0 on
-        return n >= 8 ? 0xffu : n <= 0 ? 0u : (1u << n) - 1u;
+        return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
     }
-    const int j = slot0 - st.base, w = j >> 5;                         // bits j .. j + 7, set in front of the mask, clear behind it
+    const int j = slot0 - st.base, w = j >> 5;                         // bits j .. j + 31, set in front of the mask, clear behind it
     const uint32_t* mask = a.tree + (size_t)(st.row0 + i) * a.mask_words;
     const uint32_t lo = w < 0 ? 0xffffffffu : w < a.mask_words ? mask[w] : 0u;
     const uint32_t hi = w + 1 < 0 ? 0xffffffffu : w + 1 < a.mask_words ? mask[w + 1] : 0u;
-    return (uint32_t)((((uint64_t)hi << 32) | lo) >> (j & 31)) & 0xffu;
+    return (uint32_t)((((uint64_t)hi << 32) | lo) >> (j & 31));
 }
+// the bits of the keys that lanes of group g hold, in the order of their scores
+__device__ __forceinline__ uint32_t bits_of_group(uint32_t bits, int g) { return (bits >> (4 * g) & 0xfu) | (bits >> (16 + 4 * g) & 0xfu) << 4; }
+// where score e of group g stands in its block
+__device__ __forceinline__ constexpr int key_of_score(int g, int e) { return 16 * (e >> 2) + 4 * g + (e & 3); }
 
 // ---- running softmax and sum of one tile of 16 rows ----
 template <class S>
@@ -308,7 +311,7 @@ struct RowState {
 #pragma unroll
         for (int d = 0; d < S::DTL; ++d) o[d] *= f;
     }
-    // s: scores of keys 8 g + e; on return their probabilities
+    // s: a lane's scores; on return their probabilities
     __device__ __forceinline__ void probabilities(float (&s)[8]) {
         float top = s[0];
 #pragma unroll
@@ -505,12 +508,10 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         KeyLoads<S> keys;
         ValueLoads<S> values;
         int lo = -1, hi = -1;                                          // where the current block lies
-        float4 ks[2], vs[2];                                           // int8: scales of keys 8 g .. 8 g + 7
+        float4 ks[2], vs[2];                                           // int8: scales of this lane's keys
         auto scales = [&](const float* pool, int x_lo, int x_hi, float4 (&f)[2]) {
-            const int r = (g >> 1) ? x_hi : x_lo;
-            const float* y = pool + (r < 0 ? 0 : r) + (g & 1) * 8;
-            f[0] = reinterpret_cast<const float4*>(y)[0];
-            f[1] = reinterpret_cast<const float4*>(y)[1];
+            f[0] = *reinterpret_cast<const float4*>(pool + (x_lo < 0 ? 0 : x_lo) + (unsigned)(4 * g));
+            f[1] = *reinterpret_cast<const float4*>(pool + (x_hi < 0 ? 0 : x_hi) + (unsigned)(4 * g));
         };
         int t = first + wave, ahead = 0;
         if (t < last) {
@@ -570,14 +571,14 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
                 if (lo < 0) there &= 0xffff0000u;
                 if (hi < 0) there &= 0x0000ffffu;
                 if (there != 0xffffffffu) clear_rows<S>(lds, lane, there);
-                const uint32_t mine = there >> (8 * g) & 0xffu;
+                const uint32_t mine = bits_of_group(there, g);
                 if constexpr (DT == BRL_I8) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) vf[e] = mine >> e & 1u ? vf[e] : 0.f;
                 }
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
-                    const uint32_t bits = mine & visible_bits(a, st, token[r], slot0 + 8 * g);
+                    const uint32_t bits = mine & bits_of_group(visible_bits(a, st, token[r], slot0), g);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[r][e] = bits >> e & 1u ? s[r][e] : -INFINITY;
                 }
@@ -590,9 +591,9 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
                     if (r * 16 + c < rows) {
-                        float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_pad + r * 16 + c) * p.ld_scores + slot0 + 8 * g;
+                        float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_pad + r * 16 + c) * p.ld_scores + slot0 + 4 * g;
                         reinterpret_cast<float4*>(f)[0] = make_float4(s[r][0], s[r][1], s[r][2], s[r][3]);
-                        reinterpret_cast<float4*>(f)[1] = make_float4(s[r][4], s[r][5], s[r][6], s[r][7]);
+                        reinterpret_cast<float4*>(f)[4] = make_float4(s[r][4], s[r][5], s[r][6], s[r][7]);
                     }
             }
 #pragma unroll
@@ -935,7 +936,7 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
                 for (int r = 0; r < RT; ++r) acc[r] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int x = 0; x < S::KS; ++x) {
-                    const char* f = keys + lds_chunk<S>(8 * (c >> 2) + 4 * kt + (c & 3), (4 * x + g) & (S::NCH - 1));
+                    const char* f = keys + lds_chunk<S>(16 * kt + c, (4 * x + g) & (S::NCH - 1));
                     const v8h kh = __builtin_bit_cast(v8h, *reinterpret_cast<const uint4*>(f));
                     v8h kl;
                     if constexpr (S::PL == 2) kl = __builtin_bit_cast(v8h, *reinterpret_cast<const uint4*>(f + S::PLANE));
@@ -956,8 +957,8 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
                 float kf[8];
 #pragma unroll
                 for (int e = 0; e < 8; e += 4) {
-                    *reinterpret_cast<float4*>(kf + e) = *reinterpret_cast<const float4*>(&s_scale[buf][8 * g + e]);
-                    *reinterpret_cast<float4*>(vf + e) = *reinterpret_cast<const float4*>(&s_scale[buf][32 + 8 * g + e]);
+                    *reinterpret_cast<float4*>(kf + e) = *reinterpret_cast<const float4*>(&s_scale[buf][key_of_score(0, e) + 4 * g]);
+                    *reinterpret_cast<float4*>(vf + e) = *reinterpret_cast<const float4*>(&s_scale[buf][32 + key_of_score(0, e) + 4 * g]);
                 }
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
@@ -965,10 +966,10 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
                     for (int e = 0; e < 8; ++e) s[r][e] *= kf[e];
             }
             if (t * 32 + 32 > all_see || lo[0] < 0 || hi[0] < 0) {
-                const uint32_t mine = there_of(t, lo[0], hi[0]) >> (8 * g) & 0xffu;
+                const uint32_t mine = bits_of_group(there_of(t, lo[0], hi[0]), g);
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
-                    const uint32_t bits = mine & visible_bits(a, st, token[r], t * 32 + 8 * g);
+                    const uint32_t bits = mine & bits_of_group(visible_bits(a, st, token[r], t * 32), g);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[r][e] = bits >> e & 1u ? s[r][e] : -INFINITY;
                 }
@@ -1075,17 +1076,15 @@ __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAtten
     raw.request(a.c.k, lo, hi, lane);
     float kf[8];
     if constexpr (DT == BRL_I8) {
-        const int r = (g >> 1) ? hi : lo;
-        const float* f = a.c.ks + (r < 0 ? 0 : r) + (g & 1) * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) kf[e] = f[e];
+        for (int e = 0; e < 8; ++e) kf[e] = a.c.ks[((e < 4 ? lo : hi) < 0 ? 0 : (e < 4 ? lo : hi)) + 4 * g + (e & 3)];
     }
     v8h key[2][S::KS][S::PL];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int s = 0; s < S::KS; ++s) raw.fragment(t, s, lane, key[t][s]);
-    const uint32_t mine = there >> (8 * g) & 0xffu;
+    const uint32_t mine = bits_of_group(there, g);
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const int token0 = a.tree || slot0 <= st.base ? 0 : slot0 - st.base;          // the first token that sees the block's first slot
     for (int rt = token0 * p.group / 16; rt * 16 < rows; ++rt) {
@@ -1105,7 +1104,7 @@ __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAtten
         }
         const int token = (r < rows ? r : rows - 1) / p.group;
         uint32_t bits = mine;
-        if (slot0 + 32 > st.base + (a.tree ? 0 : rt * 16 / p.group + 1)) bits &= visible_bits(a, st, token, slot0 + 8 * g);
+        if (slot0 + 32 > st.base + (a.tree ? 0 : rt * 16 / p.group + 1)) bits &= bits_of_group(visible_bits(a, st, token, slot0), g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             float x = acc[e >> 2][e & 3];
@@ -1113,7 +1112,7 @@ __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAtten
             sum[e] += bits >> e & 1u ? __builtin_amdgcn_exp2f(x - lse) : 0.f;
         }
     }
-    float* y = a.weights + (size_t)unit * a.ld_weights + slot0 + 8 * g;
+    float* y = a.weights + (size_t)unit * a.ld_weights + slot0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         float x = sum[e];
@@ -1121,7 +1120,7 @@ __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAtten
         x += lane_exchange<DPP_XOR2>(x);
         x += lane_exchange<DPP_HALF_MIRROR>(x);
         x += lane_exchange<DPP_MIRROR>(x);
-        if (c == 0 && mine >> e & 1u) y[e] += x;
+        if (c == 0 && mine >> e & 1u) y[key_of_score(g, e)] += x;
     }
 }
 
