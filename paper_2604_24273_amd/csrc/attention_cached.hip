@@ -334,32 +334,39 @@ struct RowState {
     }
 };
 
-// One wavefront's pass over a block: scores of RT row tiles against the block's 32 keys
+// One wavefront's pass over a block: scores of RT row tiles against the block's 32 keys.  A step at a time: left to itself the
+// compiler reads all query fragments and widens all keys first, and a third wavefront no longer fits its registers.
 template <class S, int RT>
 __device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const uint4* q, int lane, float (&s)[RT][8]) {
+    v4f acc[2][RT];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        v4f acc[RT];
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) acc[r] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < RT; ++r) acc[t][r] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int st = 0; st < S::KS; ++st) {
-            v8h f[S::PL];
-            k.fragment(t, st, lane, f);
+    for (int st = 0; st < S::KS; ++st) {
+        v8h f[2][S::PL];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const v8h qh = __builtin_bit_cast(v8h, q[((r * S::KS + st) * 2) * 64 + lane]);
-                const v8h ql = __builtin_bit_cast(v8h, q[((r * S::KS + st) * 2 + 1) * 64 + lane]);
-                if constexpr (S::PL == 2) acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[1], qh, acc[r], 0, 0, 0);
-                acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0], ql, acc[r], 0, 0, 0);
-                acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[0], qh, acc[r], 0, 0, 0);
+        for (int t = 0; t < 2; ++t) k.fragment(t, st, lane, f[t]);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const v8h qh = __builtin_bit_cast(v8h, q[((r * S::KS + st) * 2) * 64 + lane]);
+            const v8h ql = __builtin_bit_cast(v8h, q[((r * S::KS + st) * 2 + 1) * 64 + lane]);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if constexpr (S::PL == 2) acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][1], qh, acc[t][r], 0, 0, 0);
+                acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][0], ql, acc[t][r], 0, 0, 0);
+                acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][0], qh, acc[t][r], 0, 0, 0);
             }
         }
+        if (st % 2) __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[r][4 * t + j] = acc[r][j];
-    }
+            for (int j = 0; j < 4; ++j) s[r][4 * t + j] = acc[t][r][j];
 }
 
 template <class S, int RT>
@@ -433,9 +440,9 @@ __device__ __forceinline__ Prefix prefix_blocks(const CachedAttention& a, int la
     p.total = lane_value(x, 63);
     return p;
 }
-__device__ __forceinline__ int share_of(const Plan& p, long long entries) {
-    const long long s = (entries + p.groups - 1) / p.groups;
-    return s < p.least ? p.least : (int)s;
+__device__ __forceinline__ unsigned share_of(const Plan& p, unsigned entries) {       // (the list has fewer than 2^31)
+    const unsigned s = (entries + p.groups - 1) / p.groups;
+    return s < (unsigned)p.least ? p.least : s;
 }
 
 // ---- few rows: every wavefront of a workgroup walks its own blocks ----
@@ -453,36 +460,34 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
     char* lds = lds_all + wave * S::LDS;
 
     // this workgroup's entries: left of them, the state and head they begin in, the block in it
-    int b, h, block;
-    long long left;
+    int b, h, block, left;
     if (p.groups == 0) {
         h = blockIdx.x % a.c.n_kv; b = blockIdx.x / a.c.n_kv; block = 0;
-        left = 1ll << 40;
+        left = 0x7fffffff;
     } else {
         const Prefix pre = prefix_blocks(a, lane);
-        const long long entries = (long long)pre.total * a.c.n_kv;
-        const int share = share_of(p, entries);
-        long long at = (long long)blockIdx.x * share;
-        left = entries - at < share ? entries - at : share;
-        if (left <= 0) return;
-        const unsigned long long in = __ballot((long long)pre.before * a.c.n_kv <= at);
+        const unsigned entries = (unsigned)pre.total * a.c.n_kv, share = share_of(p, entries);
+        if (blockIdx.x > (entries - 1) / share || entries == 0) return;
+        unsigned at = blockIdx.x * share;
+        left = (int)(entries - at < share ? entries - at : share);
+        const unsigned long long in = __ballot((unsigned)pre.before * a.c.n_kv <= at);
         const int l = 63 - __builtin_clzll(in);                         // the last stretch that begins at or before the entry
-        at -= (long long)lane_value(pre.before, l) * a.c.n_kv;
+        at -= (unsigned)lane_value(pre.before, l) * a.c.n_kv;
         b = l * pre.stretch;
-        int n = state_blocks(a, b);
-        while (at >= (long long)n * a.c.n_kv) {
-            at -= (long long)n * a.c.n_kv;
+        unsigned n = state_blocks(a, b);
+        while (at >= n * a.c.n_kv) {
+            at -= n * a.c.n_kv;
             n = state_blocks(a, ++b);
         }
-        h = (int)(at / n);
-        block = (int)(at % n);
+        h = at / n;
+        block = at % n;
     }
     bool before = true;                                                // nothing but this segment's beginning lies in front
     for (;;) {
         const StateTokens st = state_tokens(a.t, a.c, b);
         const int rows = st.n * p.group, seen = st.len;                // (the last token sees them all, or bits of the mask)
         const int blocks = rows ? (seen + 31) >> 5 : 0;
-        const int first = block, last = left < blocks - block ? block + (int)left : blocks;
+        const int first = block, last = left < blocks - block ? block + left : blocks;
         if (rows) {
         const bool all = first == 0 && last == blocks;
         QueryJob<S> q;
@@ -685,11 +690,11 @@ __global__ __launch_bounds__(256) void cached_join_kernel(CachedAttention a, Pla
     if (r >= st.n * p.group) return;
     const int lane = threadIdx.x & 63;
     const Prefix pre = prefix_blocks(a, lane);
-    const int share = share_of(p, (long long)pre.total * a.c.n_kv);
-    long long start = lane_value(pre.before, b / pre.stretch);
+    const unsigned share = share_of(p, (unsigned)pre.total * a.c.n_kv);
+    unsigned start = lane_value(pre.before, b / pre.stretch);
     for (int x = b / pre.stretch * pre.stretch; x < b; ++x) start += state_blocks(a, x);
     const int blocks = (st.len + 31) >> 5;
-    start = start * a.c.n_kv + (long long)h * blocks;
+    start = start * a.c.n_kv + (unsigned)h * blocks;
     float* y = out_row(a, st, h, p.group, r);
     const int d = threadIdx.x % LANES * 4, part = threadIdx.x / LANES;
     if (blocks == 0) {
@@ -697,16 +702,16 @@ __global__ __launch_bounds__(256) void cached_join_kernel(CachedAttention a, Pla
         if (p.lse && threadIdx.x == 0) p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + r] = INFINITY;
         return;
     }
-    const int w0 = (int)(start / share), w1 = (int)((start + blocks - 1) / share);
+    const unsigned w0 = start / share, w1 = (start + blocks - 1) / share;
     if (w0 == w1) return;                                              // written by that workgroup
-    auto slot = [&](int w) { return (2 * (size_t)w + (w == w0 && start > (long long)w * share ? 1 : 0)) * p.rows_pad + r; };
+    auto slot = [&](unsigned w) { return (2 * (size_t)w + (w == w0 && start > w * share ? 1 : 0)) * p.rows_pad + r; };
     float ref = -INFINITY;
-    for (int w = w0 + lane; w <= w1; w += 64) ref = fmaxf(ref, p.part_ml[slot(w)].x);
+    for (unsigned w = w0 + lane; w <= w1; w += 64) ref = fmaxf(ref, p.part_ml[slot(w)].x);
     ref = wave_max(ref);
     float l = 0.f;
     v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int w = w0 + part; w <= w1; w += PARTS) {
+    for (unsigned w = w0 + part; w <= w1; w += PARTS) {
         const float2 ml = p.part_ml[slot(w)];
         const v4f x = d < DH ? *reinterpret_cast<const v4f*>(p.part_o + slot(w) * DH + d) : v4f{0.f, 0.f, 0.f, 0.f};
         const float f = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
@@ -1146,7 +1151,7 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
         p.rows_pad = L.rt * 16;
         // One workgroup of eight wavefronts per (state, k/v head) where that is a few blocks for each of them: no second launch.
         // So, too, where there are far more of them than workgroups at a time.
-        if (blocks <= 32 || (long long)units * p.rows_max > (1 << 22)) {
+        if (blocks <= 32 || (long long)units * p.rows_max > (1 << 22) || (long long)units * blocks >= (1ll << 31)) {
             L.waves = 8;
         } else {
             L.waves = 4;
