@@ -1149,14 +1149,18 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
     if (!L.tiles) {
         L.rt = p.rows_max <= 16 ? 1 : 2;
         p.rows_pad = L.rt * 16;
-        // One workgroup of eight wavefronts per (state, k/v head) where that is a few blocks for each of them: no second launch.
-        // So, too, where there are far more of them than workgroups at a time.
-        if (blocks <= 32 || (long long)units * p.rows_max > (1 << 22) || (long long)units * blocks >= (1ll << 31)) {
-            L.waves = 8;
+        // A workgroup per (state, k/v head) needs no second launch (about 7 us) but takes all of a state's keys through one compute unit:
+        // up to two turns of its eight wavefronts of an fp32 cache, four of the others, which are half the work, twice that
+        // where there are workgroups to fill every unit.  5 heads of 128 and 1000 slots, this form / shared: fp16 14.0 / 13.8 us,
+        // fp32 23.0 / 17.2, 512 slots 12.2 / 18.6 and 19.5 / 23.1; 1280 of 1000: fp16 116 / 126; 5 of 2000: 18.4 / 13.8.
+        const int whole = c.dtype == BRL_F32 ? 16 : 32;
+        if (blocks <= whole || (units >= 512 && blocks <= 64) || (long long)units * p.rows_max > (1 << 22) ||
+            (long long)units * blocks >= (1ll << 31)) {
+            L.waves = blocks <= 4 || units >= 2048 ? 4 : 8;
         } else {
             L.waves = 4;
-            p.groups = 512;
-            p.least = 8;
+            p.groups = 512;                           // as many as run at a time
+            p.least = 4;
         }
         parts = 2 * (size_t)p.groups * p.rows_pad;
     } else {
