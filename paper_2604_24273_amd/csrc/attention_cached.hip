@@ -262,24 +262,6 @@ struct QueryPart {
         split_pair(z[6], z[7], hi.w, lo.w);
     }
 };
-// The same as a job: one lane of one (row tile, step) of fragments in LDS, [row tile][step][hi, lo][64 lanes].
-template <class S>
-struct QueryJob {
-    QueryPart<S> part;
-    __device__ __forceinline__ void request(const CachedAttention& a, const StateTokens& st, int h, int group, int rows, int job) {
-        const int lane = job & 63, r = (job >> 6) / S::KS * 16 + (lane & 15);
-        const QueryRow q(a, st, h, group, r < rows ? r : rows - 1);
-        part.request(q.x, q.ct, q.sn, 32 * ((job >> 6) % S::KS) + 8 * (lane >> 4));
-    }
-    __device__ __forceinline__ void store(uint4* lds, int rows, int job) const {
-        const int lane = job & 63, s = (job >> 6) % S::KS, rt = (job >> 6) / S::KS;
-        uint4 hi, lo;
-        part.split(rt * 16 + (lane & 15) < rows, 32 * s + 8 * (lane >> 4), hi, lo);
-        lds[((rt * S::KS + s) * 2) * 64 + lane] = hi;
-        lds[((rt * S::KS + s) * 2 + 1) * 64 + lane] = lo;
-    }
-};
-
 // which of the slots slot0 .. slot0 + 31 token i sees, for blocks that not every row sees whole
 __device__ __forceinline__ uint32_t visible_bits(const CachedAttention& a, const StateTokens& st, int i, int slot0) {
     if (!a.tree) {
@@ -334,43 +316,31 @@ struct RowState {
     }
 };
 
-// One wavefront's pass over a block: scores of RT row tiles against the block's 32 keys.  A step at a time: left to itself the
-// compiler reads all query fragments and widens all keys first, and a third wavefront no longer fits its registers.
-template <class S, int RT>
-__device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const uint4* q, int lane, float (&s)[RT][8]) {
-    v4f acc[2][RT];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < RT; ++r) acc[t][r] = v4f{0.f, 0.f, 0.f, 0.f};
+// One wavefront's pass over a block: scores of 16 rows against the block's 32 keys.  A step at a time: left to itself the compiler
+// reads all query fragments and widens all keys first.
+template <class S>
+__device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const uint4* q, int lane, float (&s)[8]) {
+    v4f acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int st = 0; st < S::KS; ++st) {
         v8h f[2][S::PL];
 #pragma unroll
         for (int t = 0; t < 2; ++t) k.fragment(t, st, lane, f[t]);
+        const v8h qh = __builtin_bit_cast(v8h, q[(st * 2) * 64 + lane]), ql = __builtin_bit_cast(v8h, q[(st * 2 + 1) * 64 + lane]);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const v8h qh = __builtin_bit_cast(v8h, q[((r * S::KS + st) * 2) * 64 + lane]);
-            const v8h ql = __builtin_bit_cast(v8h, q[((r * S::KS + st) * 2 + 1) * 64 + lane]);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if constexpr (S::PL == 2) acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][1], qh, acc[t][r], 0, 0, 0);
-                acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][0], ql, acc[t][r], 0, 0, 0);
-                acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][0], qh, acc[t][r], 0, 0, 0);
-            }
+        for (int t = 0; t < 2; ++t) {
+            if constexpr (S::PL == 2) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][1], qh, acc[t], 0, 0, 0);
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][0], ql, acc[t], 0, 0, 0);
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[t][0], qh, acc[t], 0, 0, 0);
         }
         if (st % 2) __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[r][4 * t + j] = acc[t][r][j];
+    for (int e = 0; e < 8; ++e) s[e] = acc[e >> 2][e & 3];
 }
 
 template <class S, int RT>
-__device__ __forceinline__ void block_values(const char* lds, const float (&p)[RT][8], RowState<S> (&st)[RT], int lane) {
+__device__ __forceinline__ void block_values(const char* lds, const float (*p)[8], RowState<S>* st, int lane) {
     v8h ph[RT], pl[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -449,12 +419,12 @@ __device__ __forceinline__ unsigned share_of(const Plan& p, unsigned entries) { 
 // Nothing is shared between wavefronts but the query rows: keys go from memory into operand registers, values through a region of
 // LDS of the wavefront's own, where the transposing reads turn them.  The next block's keys are requested as soon as the scores
 // have been taken, its values as soon as this block's have been stored, so that loads are in flight all the time.
-template <int DT, int DH, int RT>
+template <int DT, int DH>
 __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a, Plan p) {
     typedef Shape<DT, DH> S;
     extern __shared__ __attribute__((aligned(16))) char lds_all[];
-    __shared__ uint4 s_q[RT * S::KS * 2 * 64];
-    __shared__ float2 s_ml[8][RT * 16];
+    __shared__ uint4 s_q[S::KS * 2 * 64];                              // query fragments: [step][hi, lo][64 lanes]
+    __shared__ float2 s_ml[8][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int c = lane & 15, g = lane >> 4;
     char* lds = lds_all + wave * S::LDS;
@@ -490,18 +460,19 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         const int first = block, last = left < blocks - block ? block + left : blocks;
         if (rows) {
         const bool all = first == 0 && last == blocks;
-        QueryJob<S> q;
-        constexpr int JOBS = RT * S::KS * 64;
-        static_assert(JOBS <= 512, "two jobs a thread at most");
-        if (threadIdx.x < JOBS) q.request(a, st, h, p.group, rows, threadIdx.x);
-        RowState<S> row[RT];
-        float unit = 0x1p126f;                                         // int8: power of two that the sums are multiplied by
-        int token[RT];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            row[r].clear();
-            token[r] = (r * 16 + c < rows ? r * 16 + c : rows - 1) / p.group;
+        QueryPart<S> q;
+        constexpr int JOBS = S::KS * 64;                               // a lane of a step's fragment each, of the first threads
+        static_assert(JOBS <= 256, "every workgroup has the threads");
+        const bool live = c < rows;
+        const int d0 = 32 * wave + 8 * g;
+        if (threadIdx.x < JOBS) {
+            const QueryRow from(a, st, h, p.group, live ? c : rows - 1);
+            q.request(from.x, from.ct, from.sn, d0);
         }
+        RowState<S> row;
+        float unit = 0x1p126f;                                         // int8: power of two that the sums are multiplied by
+        row.clear();
+        const int token = (live ? c : rows - 1) / p.group;
         const int all_see = st.base + (a.tree ? 0 : 1);                // slots below are seen by every row (causal: by token 0)
 
         int page_lo = -1, page_hi = -1;                                // rows of the lane-th block ahead
@@ -528,27 +499,23 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
             values.request(a.c.v, lo, hi, lane);
             if constexpr (DT == BRL_I8) scales(a.c.vs, lo, hi, vs);
         }
-        if (threadIdx.x < JOBS) q.store(s_q, rows, threadIdx.x);
-        if constexpr (JOBS > 256) {
-            const int job = blockDim.x + threadIdx.x;
-            if (job < JOBS) {
-                q.request(a, st, h, p.group, rows, job);
-                q.store(s_q, rows, job);
-            }
+        if (threadIdx.x < JOBS) {
+            uint4 x, y;
+            q.split(live, d0, x, y);
+            s_q[2 * wave * 64 + lane] = x;
+            s_q[(2 * wave + 1) * 64 + lane] = y;
         }
         __syncthreads();
         for (; t < last; t += waves) {
             const int slot0 = t * 32;
             int at = lane;                                             // (opaque: or the compiler keeps all of LDS in registers)
             asm volatile("" : "+v"(at));
-            float s[RT][8];
-            block_scores<S, RT>(keys, s_q, at, s);
+            float s[8];
+            block_scores<S>(keys, s_q, at, s);
             if constexpr (DT == BRL_I8) {
                 const float f[8] = {ks[0].x, ks[0].y, ks[0].z, ks[0].w, ks[1].x, ks[1].y, ks[1].z, ks[1].w};
 #pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s[r][e] *= f[e];
+                for (int e = 0; e < 8; ++e) s[e] *= f[e];
             }
             __builtin_amdgcn_sched_barrier(0);                         // (the old keys' registers are free from here on)
             // Behind the last block, rows 0 of the pool are requested and never used: a request that might not be made would
@@ -581,28 +548,20 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
 #pragma unroll
                     for (int e = 0; e < 8; ++e) vf[e] = mine >> e & 1u ? vf[e] : 0.f;
                 }
+                const uint32_t bits = mine & bits_of_group(visible_bits(a, st, token, slot0), g);
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    const uint32_t bits = mine & bits_of_group(visible_bits(a, st, token[r], slot0), g);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s[r][e] = bits >> e & 1u ? s[r][e] : -INFINITY;
-                }
+                for (int e = 0; e < 8; ++e) s[e] = bits >> e & 1u ? s[e] : -INFINITY;
             }
             __builtin_amdgcn_sched_barrier(0);
             values.request(a.c.v, next_lo, next_hi, lane);
             if constexpr (DT == BRL_I8) scales(a.c.vs, next_lo, next_hi, vs);
             __builtin_amdgcn_sched_barrier(0);
-            if (p.scores) {
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-                    if (r * 16 + c < rows) {
-                        float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_pad + r * 16 + c) * p.ld_scores + slot0 + 4 * g;
-                        reinterpret_cast<float4*>(f)[0] = make_float4(s[r][0], s[r][1], s[r][2], s[r][3]);
-                        reinterpret_cast<float4*>(f)[4] = make_float4(s[r][4], s[r][5], s[r][6], s[r][7]);
-                    }
+            if (p.scores && live) {
+                float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_pad + c) * p.ld_scores + slot0 + 4 * g;
+                reinterpret_cast<float4*>(f)[0] = make_float4(s[0], s[1], s[2], s[3]);
+                reinterpret_cast<float4*>(f)[4] = make_float4(s[4], s[5], s[6], s[7]);
             }
-#pragma unroll
-            for (int r = 0; r < RT; ++r) row[r].probabilities(s[r]);
+            row.probabilities(s);
             if constexpr (DT == BRL_I8) {
                 // scales relative to the largest so far, a power of two that only falls: fp16 holds the products
                 float top = vf[0];
@@ -611,62 +570,52 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
                 if (__any(top * unit > 1.f)) {
                     const float now = __builtin_amdgcn_exp2f(-ceilf(__builtin_amdgcn_logf(wave_max(top))) - 1.f);
                     const float f = now / unit;
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) row[r].scale(f);
+                    row.scale(f);
                     unit = now;
                 }
 #pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s[r][e] *= vf[e] * unit;
+                for (int e = 0; e < 8; ++e) s[e] *= vf[e] * unit;
             }
             __builtin_amdgcn_wave_barrier();
-            block_values<S, RT>(lds, s, row, at);
+            block_values<S, 1>(lds, &s, &row, at);
             __builtin_amdgcn_wave_barrier();
             lo = next_lo;
             hi = next_hi;
         }
-        // the wavefronts' parts meet: sums to the largest reference, then O over LDS, a row tile at a time
+        // the wavefronts' parts meet: sums to the largest reference, then O over LDS
+        row.l += __shfl_xor(row.l, 16, 64);
+        row.l += __shfl_xor(row.l, 32, 64);
+        if (g == 0) s_ml[wave][c] = make_float2(row.l > 0.f ? row.ref : -INFINITY, row.l);
+        __syncthreads();
+        float top = -INFINITY;
+        for (int w = 0; w < waves; ++w) top = fmaxf(top, s_ml[w][c].x);
+        float f = row.l > 0.f ? __builtin_amdgcn_exp2f(row.ref - top) : 0.f;
+        if constexpr (DT == BRL_I8) f /= unit;
+        float* o = reinterpret_cast<float*>(lds);                      // [16 rows][ROW]
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            row[r].l += __shfl_xor(row[r].l, 16, 64);
-            row[r].l += __shfl_xor(row[r].l, 32, 64);
-            if (g == 0) s_ml[wave][r * 16 + c] = make_float2(row[r].l > 0.f ? row[r].ref : -INFINITY, row[r].l);
+        for (int d = 0; d < S::DTL; ++d) *reinterpret_cast<v4f*>(o + c * S::ROW + 16 * d + 4 * g) = row.o[d] * f;
+        __syncthreads();
+        const size_t slot = (2 * (size_t)blockIdx.x + (before ? 0 : 1)) * p.rows_pad;
+        for (int i = threadIdx.x; i < 16 * S::ROW / 4; i += blockDim.x) {
+            const int r = i / (S::ROW / 4), d = i % (S::ROW / 4) * 4;
+            if (r >= rows || d >= DH) continue;
+            float ref = -INFINITY, l = 0.f;
+            for (int w = 0; w < waves; ++w) ref = fmaxf(ref, s_ml[w][r].x);
+            v4f sum = {0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < waves; ++w) {
+                const float2 ml = s_ml[w][r];
+                if (ml.y > 0.f) l += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
+                sum += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds_all + w * S::LDS) + r * S::ROW + d);
+            }
+            if (all) {
+                *reinterpret_cast<v4f*>(out_row(a, st, h, p.group, r) + d) = sum * (l > 0.f ? 1.f / l : 0.f);
+                if (p.lse && d == 0) p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + r] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
+            } else {
+                *reinterpret_cast<v4f*>(p.part_o + (slot + r) * DH + d) = sum;
+                if (d == 0) p.part_ml[slot + r] = make_float2(ref, l);
+            }
         }
         __syncthreads();
-        const size_t slot = 2 * (size_t)blockIdx.x + (before ? 0 : 1);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            float top = -INFINITY;
-            for (int w = 0; w < waves; ++w) top = fmaxf(top, s_ml[w][r * 16 + c].x);
-            float f = row[r].l > 0.f ? __builtin_amdgcn_exp2f(row[r].ref - top) : 0.f;
-            if constexpr (DT == BRL_I8) f /= unit;
-            float* o = reinterpret_cast<float*>(lds);                  // [16 rows][ROW]
-#pragma unroll
-            for (int d = 0; d < S::DTL; ++d) *reinterpret_cast<v4f*>(o + c * S::ROW + 16 * d + 4 * g) = row[r].o[d] * f;
-            __syncthreads();
-            for (int i = threadIdx.x; i < 16 * S::ROW / 4; i += blockDim.x) {
-                const int x = i / (S::ROW / 4), d = i % (S::ROW / 4) * 4, rr = r * 16 + x;
-                if (rr >= rows || d >= DH) continue;
-                float ref = -INFINITY, l = 0.f;
-                for (int w = 0; w < waves; ++w) ref = fmaxf(ref, s_ml[w][rr].x);
-                v4f sum = {0.f, 0.f, 0.f, 0.f};
-                for (int w = 0; w < waves; ++w) {
-                    const float2 ml = s_ml[w][rr];
-                    if (ml.y > 0.f) l += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
-                    sum += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds_all + w * S::LDS) + x * S::ROW + d);
-                }
-                if (all) {
-                    *reinterpret_cast<v4f*>(out_row(a, st, h, p.group, rr) + d) = sum * (l > 0.f ? 1.f / l : 0.f);
-                    if (p.lse && d == 0)
-                        p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + rr] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
-                } else {
-                    *reinterpret_cast<v4f*>(p.part_o + (slot * p.rows_pad + rr) * DH + d) = sum;
-                    if (d == 0) p.part_ml[slot * p.rows_pad + rr] = make_float2(ref, l);
-                }
-            }
-            __syncthreads();
-        }
         }
         if (p.groups == 0) return;
         left -= last - first;
@@ -680,11 +629,57 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
     }
 }
 
-// ---- the parts of a (state, k/v head) that several workgroups took, joined: a workgroup per row ----
+// ---- parts of a row's keys joined ----
+// 256 threads: four components of the row each, LANES of them; the rest of the threads share the parts, or are other rows.
+template <int DH, int GROUPS>
+struct Joiner {
+    static constexpr int LANES = DH == 100 ? 32 : DH / 4, PER = 256 / LANES;
+    static_assert(GROUPS == 1 || GROUPS == PER, "all on one row, or each on its own");
+    // parts w0 .. w1 at place(w) of part_ml and part_o
+    template <class Place>
+    static __device__ __forceinline__ void run(const Plan& p, unsigned w0, unsigned w1, Place place, float* y, float* lse) {
+        __shared__ __attribute__((aligned(16))) float s_o[PER][DH];
+        __shared__ float s_l[PER];
+        const int d = threadIdx.x % LANES * 4, part = threadIdx.x / LANES;
+        float ref = -INFINITY;
+        if constexpr (GROUPS == 1) {
+            for (unsigned w = w0 + (threadIdx.x & 63); w <= w1; w += 64) ref = fmaxf(ref, p.part_ml[place(w)].x);
+            ref = wave_max(ref);
+        } else {
+            for (unsigned w = w0; w <= w1; ++w) ref = fmaxf(ref, p.part_ml[place(w)].x);
+        }
+        float l = 0.f;
+        v4f o = {0.f, 0.f, 0.f, 0.f};
+        constexpr unsigned STEP = GROUPS == 1 ? PER : 1;
+#pragma unroll 4
+        for (unsigned w = w0 + (GROUPS == 1 ? part : 0); w <= w1; w += STEP) {
+            const float2 ml = p.part_ml[place(w)];
+            const v4f x = d < DH ? *reinterpret_cast<const v4f*>(p.part_o + place(w) * DH + d) : v4f{0.f, 0.f, 0.f, 0.f};
+            const float f = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
+            l += ml.y * f;
+            o += x * f;
+        }
+        if constexpr (GROUPS == 1) {
+            if (d < DH) *reinterpret_cast<v4f*>(&s_o[part][d]) = o;
+            if (d == 0) s_l[part] = l;
+            __syncthreads();
+            if (part != 0) return;
+            l = 0.f;
+            o = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                l += s_l[x];
+                if (d < DH) o += *reinterpret_cast<const v4f*>(&s_o[x][d]);
+            }
+        }
+        if (d < DH) *reinterpret_cast<v4f*>(y + d) = o * (l > 0.f ? 1.f / l : 0.f);
+        if (lse && d == 0) *lse = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
+    }
+};
+
+// few rows: the parts that workgroups of the shared list took, a workgroup per row
 template <int DH>
 __global__ __launch_bounds__(256) void cached_join_kernel(CachedAttention a, Plan p) {
-    constexpr int LANES = DH == 100 ? 32 : DH / 4, PARTS = 256 / LANES;
-    __shared__ __attribute__((aligned(16))) float s_o[PARTS][DH];
     const int r = blockIdx.x % p.rows_max, h = blockIdx.x / p.rows_max % a.c.n_kv, b = blockIdx.x / p.rows_max / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
     if (r >= st.n * p.group) return;
@@ -696,42 +691,28 @@ __global__ __launch_bounds__(256) void cached_join_kernel(CachedAttention a, Pla
     const int blocks = (st.len + 31) >> 5;
     start = start * a.c.n_kv + (unsigned)h * blocks;
     float* y = out_row(a, st, h, p.group, r);
-    const int d = threadIdx.x % LANES * 4, part = threadIdx.x / LANES;
-    if (blocks == 0) {
-        if (part == 0 && d < DH) *reinterpret_cast<v4f*>(y + d) = v4f{0.f, 0.f, 0.f, 0.f};
-        if (p.lse && threadIdx.x == 0) p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + r] = INFINITY;
+    float* lse = p.lse ? p.lse + ((size_t)b * a.c.n_kv + h) * p.rows_pad + r : nullptr;
+    if (blocks == 0) {                                                 // no workgroup of the list comes by
+        if (threadIdx.x < DH) y[threadIdx.x] = 0.f;
+        if (lse && threadIdx.x == 0) *lse = INFINITY;
         return;
     }
     const unsigned w0 = start / share, w1 = (start + blocks - 1) / share;
     if (w0 == w1) return;                                              // written by that workgroup
-    auto slot = [&](unsigned w) { return (2 * (size_t)w + (w == w0 && start > w * share ? 1 : 0)) * p.rows_pad + r; };
-    float ref = -INFINITY;
-    for (unsigned w = w0 + lane; w <= w1; w += 64) ref = fmaxf(ref, p.part_ml[slot(w)].x);
-    ref = wave_max(ref);
-    float l = 0.f;
-    v4f o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (unsigned w = w0 + part; w <= w1; w += PARTS) {
-        const float2 ml = p.part_ml[slot(w)];
-        const v4f x = d < DH ? *reinterpret_cast<const v4f*>(p.part_o + slot(w) * DH + d) : v4f{0.f, 0.f, 0.f, 0.f};
-        const float f = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
-        l += ml.y * f;
-        o += x * f;
-    }
-    __shared__ float s_l[PARTS];
-    if (d < DH) *reinterpret_cast<v4f*>(&s_o[part][d]) = o;
-    if (d == 0) s_l[part] = l;
-    __syncthreads();
-    if (part != 0 || d >= DH) return;
-    l = 0.f;
-    o = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int x = 0; x < PARTS; ++x) {
-        l += s_l[x];
-        o += *reinterpret_cast<const v4f*>(&s_o[x][d]);
-    }
-    *reinterpret_cast<v4f*>(y + d) = o * (l > 0.f ? 1.f / l : 0.f);
-    if (p.lse && d == 0) p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + r] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
+    Joiner<DH, 1>::run(p, w0, w1, [&](unsigned w) { return (2 * (size_t)w + (w == w0 && start > w * share ? 1 : 0)) * p.rows_pad + r; }, y, lse);
+}
+
+// many rows: a fixed number of parts; a workgroup for several rows where they are few
+template <int DH, int GROUPS>
+__global__ __launch_bounds__(256) void cached_join_splits_kernel(CachedAttention a, Plan p) {
+    const long long i = (long long)blockIdx.x * GROUPS + (GROUPS == 1 ? 0 : threadIdx.x / Joiner<DH, GROUPS>::LANES);
+    const int r = (int)(i % p.rows_max), unit = (int)(i / p.rows_max), h = unit % a.c.n_kv, b = unit / a.c.n_kv;
+    if (b >= a.t.B) return;
+    const StateTokens st = state_tokens(a.t, a.c, b);
+    if (r >= st.n * p.group) return;
+    const size_t at = ((size_t)unit * p.rows_pad + r) * p.splits;
+    Joiner<DH, GROUPS>::run(p, 0u, (unsigned)p.splits - 1, [&](unsigned w) { return at + w; }, out_row(a, st, h, p.group, r),
+                            p.lse ? p.lse + (size_t)unit * p.rows_pad + r : nullptr);
 }
 
 // ---- weights of slots from the stored scores: a thread per four slots ----
@@ -1035,32 +1016,6 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
     }
 }
 
-// the parts of a row that a fixed number of workgroups took
-template <int DH>
-__global__ __launch_bounds__(64) void cached_join_splits_kernel(CachedAttention a, Plan p) {
-    const int lane = threadIdx.x, r = blockIdx.x % p.rows_max, unit = blockIdx.x / p.rows_max, h = unit % a.c.n_kv, b = unit / a.c.n_kv;
-    const StateTokens st = state_tokens(a.t, a.c, b);
-    if (r >= st.n * p.group) return;
-    const size_t at = ((size_t)unit * p.rows_pad + r) * p.splits;
-    float ref = -INFINITY;
-    for (int s = 0; s < p.splits; ++s) ref = fmaxf(ref, p.part_ml[at + s].x);
-    float l = 0.f, o[2] = {0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < p.splits; ++s) {
-        const float2 ml = p.part_ml[at + s];
-        const float f = ml.y > 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
-        const float* x = p.part_o + (at + s) * DH;
-        l += ml.y * f;
-        if (lane < DH) o[0] += x[lane] * f;
-        if (DH > 64 && lane + 64 < DH) o[1] += x[lane + 64] * f;
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    float* y = out_row(a, st, h, p.group, r);
-    if (lane < DH) y[lane] = o[0] * inv;
-    if (DH > 64 && lane + 64 < DH) y[lane + 64] = o[1] * inv;
-    if (p.lse && lane == 0) p.lse[(size_t)unit * p.rows_pad + r] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
-}
-
 // Weights of slots, many rows: the scores once more.  A wavefront keeps a block of 32 keys in registers and walks the row tiles that
 // can see it; each lane sums its eight keys over its row of every tile, the sixteen rows meet at the end.
 template <int DT, int DH>
@@ -1131,8 +1086,8 @@ __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAtten
 
 struct Layout {
     Plan p;
-    int waves, rt;            // few rows: wavefronts of a workgroup; row tiles of a wavefront
     bool tiles;               // many rows
+    int waves, rt;            // few rows: wavefronts of a workgroup; many: row tiles of a wavefront
     size_t o_off, ml_off, lse_off, scores_off, q_off, total;
 };
 
@@ -1144,11 +1099,12 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
     p.rows_max = max_new * p.group;
     p.splits = 1;
     const int units = B * c.n_kv, blocks = (max_len + 31) / 32;
-    L.tiles = p.rows_max > 32;
+    // 16 rows fill one column block of the matrix instructions; more would have a wavefront of the first form hold two.  20 rows, 64
+    // states of 1000-2000 slots, first form / second: fp16 82 / 75 us, fp32 175 / 123; 4 rows: 80 / 93 and 142 / 155.
+    L.tiles = p.rows_max > 16;
     size_t parts;
     if (!L.tiles) {
-        L.rt = p.rows_max <= 16 ? 1 : 2;
-        p.rows_pad = L.rt * 16;
+        p.rows_pad = 16;
         // A workgroup per (state, k/v head) needs no second launch (about 7 us) but takes all of a state's keys through one compute unit:
         // up to two turns of its eight wavefronts of an fp32 cache, four of the others, which are half the work, twice that
         // where there are workgroups to fill every unit.  5 heads of 128 and 1000 slots, this form / shared: fp16 14.0 / 13.8 us,
@@ -1171,8 +1127,8 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
         // have to be joined another four; the split with the shortest sum of rounds.
         const long long groups = (long long)units * p.row_blocks;
         long long best = 0;
-        for (int s = 1; s <= 16 && (s == 1 || blocks / s >= 8); ++s) {
-            const long long cost = (groups * s + 511) / 512 * ((blocks + s - 1) / s + 4) + (s > 1 ? 4 : 0);
+        for (int s = 1; s <= 64 && (s == 1 || blocks / s >= 8); ++s) {
+            const long long cost = (groups * s + 511) / 512 * ((blocks + s - 1) / s + 4) + (s > 1 ? 4 + s / 8 : 0);
             if (s == 1 || cost < best) { best = cost; p.splits = s; }
         }
         parts = p.splits > 1 ? (size_t)units * p.rows_pad * p.splits : 0;
@@ -1204,8 +1160,7 @@ int launch_few(const CachedAttention& a, const Layout& L, hipStream_t s) {
     const Plan& p = L.p;
     const dim3 grid((unsigned)(p.groups ? p.groups : a.t.B * a.c.n_kv)), block(L.waves * 64);
     const size_t lds = (size_t)L.waves * Shape<DT, DH>::LDS;
-    if (L.rt == 1) hipLaunchKernelGGL((cached_stream_kernel<DT, DH, 1>), grid, block, lds, s, a, p);
-    else hipLaunchKernelGGL((cached_stream_kernel<DT, DH, 2>), grid, block, lds, s, a, p);
+    hipLaunchKernelGGL((cached_stream_kernel<DT, DH>), grid, block, lds, s, a, p);
     BRL_LAUNCH_CHECK("cached_stream_kernel");
     if (p.groups) {
         hipLaunchKernelGGL(cached_join_kernel<DH>, dim3((unsigned)(a.t.B * a.c.n_kv * p.rows_max)), dim3(256), 0, s, a, p);
@@ -1228,7 +1183,10 @@ int launch_many(const CachedAttention& a, const Layout& L, hipStream_t s) {
     else hipLaunchKernelGGL((cached_tiles_kernel<DT, DH, 2>), grid, block, 0, s, a, p);
     BRL_LAUNCH_CHECK("cached_tiles_kernel");
     if (p.splits > 1) {
-        hipLaunchKernelGGL(cached_join_splits_kernel<DH>, dim3((unsigned)(units * p.rows_max)), dim3(64), 0, s, a, p);
+        constexpr int PER = Joiner<DH, 1>::PER;
+        const unsigned rows = (unsigned)(units * p.rows_max);
+        if (p.splits <= 4) hipLaunchKernelGGL((cached_join_splits_kernel<DH, PER>), dim3((rows + PER - 1) / PER), dim3(256), 0, s, a, p);
+        else hipLaunchKernelGGL((cached_join_splits_kernel<DH, 1>), dim3(rows), dim3(256), 0, s, a, p);
         BRL_LAUNCH_CHECK("cached_join_splits_kernel");
     }
     if (a.weights) {
