@@ -67,7 +67,7 @@ struct Shape {
 // Where chunk c of a key's row lies in LDS.  The chunks of a row are permuted by bits of the key such that both the 16 rows
 // x 16 bytes of a key fragment and the 16 rows x 32 bytes of a transposing read fall on all banks.
 template <class S>
-__device__ __forceinline__ int lds_chunk(int key, int c) {
+__device__ __forceinline__ unsigned lds_chunk(unsigned key, unsigned c) {      // (unsigned: shifts and masks, no corrections for signs)
     constexpr int SKIP = S::NCH == 16 ? 0 : S::NCH == 8 ? 1 : S::NCH == 4 ? 2 : 3;   // rows that lie side by side in 256 bytes
     return key * S::LS + ((c ^ ((key & 15) >> SKIP)) << 4);
 }
@@ -101,7 +101,7 @@ struct KeyLoads {
             }
         }
     }
-    __device__ __forceinline__ void fragment(int t, int s, int lane, v8h (&f)[S::PL]) const {
+    __device__ __forceinline__ void fragment(int t, int s, unsigned lane, v8h (&f)[S::PL]) const {
         uint32_t w[S::PL][4];
         if constexpr (S::DT == BRL_F32) {
 #pragma unroll
@@ -119,7 +119,7 @@ struct KeyLoads {
             widen_codes(r.y, w[0][2], w[0][3]);
         }
         if (S::KS * 32 > S::DH && s == S::KS - 1) {                    // what lies behind head_dim is not a number
-            const int valid = S::DH - (32 * s + 8 * (lane >> 4));
+            const int valid = S::DH - (32 * s + 8 * (int)(lane >> 4));
 #pragma unroll
             for (int p = 0; p < S::PL; ++p)
 #pragma unroll
@@ -149,11 +149,11 @@ struct ValueLoads {
             else raw[i] = *reinterpret_cast<const uint4*>(idx >= HALF ? hi + (unsigned)((idx - HALF) * 16) : lo + (unsigned)(idx * 16));
         }
     }
-    __device__ __forceinline__ void store(char* lds, int lane) const {
+    __device__ __forceinline__ void store(char* lds, unsigned lane) const {
 #pragma unroll
         for (int i = 0; i < S::NV; ++i) {
-            const int idx = i * 64 + lane, key = idx / S::CPR, c = idx % S::CPR;
-            if (S::NV * 64 > 32 * S::CPR && idx >= 32 * S::CPR) continue;
+            const unsigned idx = i * 64 + lane, key = idx / S::CPR, c = idx % S::CPR;
+            if (S::NV * 64 > 32 * S::CPR && idx >= 32u * S::CPR) continue;
             const uint4 r = raw[i];
             if constexpr (S::DT == BRL_F16) {
                 *reinterpret_cast<uint4*>(lds + lds_chunk<S>(key, c)) = r;
@@ -190,16 +190,16 @@ __device__ __forceinline__ void clear_rows(char* lds, int lane, uint32_t there) 
 template <class S>
 struct ValueReads {
     const char* base;
-    int x;
-    __device__ __forceinline__ ValueReads(const char* lds, int lane) {
-        const int c = lane & 15, key = 4 * (lane >> 4) + (c >> 2);
-        const int at = lds_chunk<S>(key, (c & 3) >> 1);
+    unsigned x;
+    __device__ __forceinline__ ValueReads(const char* lds, unsigned lane) {
+        const unsigned c = lane & 15, key = 4 * (lane >> 4) + (c >> 2);
+        const unsigned at = lds_chunk<S>(key, (c & 3) >> 1);
         base = lds + key * S::LS + (c & 1) * 8;
         x = at - key * S::LS;
     }
     __device__ __forceinline__ v8h fragment(int d, int plane) const {
         uint2 r[2];
-        const char* p = base + (x ^ (d << 5));
+        const char* p = base + (x ^ (unsigned)(d << 5));
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             typedef __attribute__((address_space(3))) v4fp* lds_ptr;
@@ -212,8 +212,10 @@ struct ValueReads {
 
 struct QueryRow {
     const float *x, *ct, *sn;          // a query row, the cosines and sines of its position
-    __device__ __forceinline__ QueryRow(const CachedAttention& a, const StateTokens& st, int h, int group, int r) {
-        const int i = r / group, row = st.row0 + i, pos = rope_position(a.t, row, st.base + i), dh = a.c.dh;
+    __device__ __forceinline__ QueryRow(const CachedAttention& a, const StateTokens& st, int h, int group, int r)
+        : QueryRow(a, st, h, group, r, rope_position(a.t, st.row0 + r / group, st.base + r / group)) {}
+    __device__ __forceinline__ QueryRow(const CachedAttention& a, const StateTokens& st, int h, int group, int r, int pos) {
+        const int i = r / group, row = st.row0 + i, dh = a.c.dh;
         x = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * dh) + (h * group + r % group) * dh;
         ct = a.t.cos_t + (size_t)pos * (dh / 2);
         sn = a.t.sin_t + (size_t)pos * (dh / 2);
@@ -319,7 +321,7 @@ struct RowState {
 // One wavefront's pass over a block: scores of 16 rows against the block's 32 keys.  A step at a time: left to itself the compiler
 // reads all query fragments and widens all keys first.
 template <class S>
-__device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const uint4* q, int lane, float (&s)[8]) {
+__device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const uint4* q, unsigned lane, float (&s)[8]) {
     v4f acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int st = 0; st < S::KS; ++st) {
@@ -340,7 +342,7 @@ __device__ __forceinline__ void block_scores(const KeyLoads<S>& k, const uint4* 
 }
 
 template <class S, int RT>
-__device__ __forceinline__ void block_values(const char* lds, const float (*p)[8], RowState<S>* st, int lane) {
+__device__ __forceinline__ void block_values(const char* lds, const float (*p)[8], RowState<S>* st, unsigned lane) {
     v8h ph[RT], pl[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -386,20 +388,23 @@ __device__ __forceinline__ float* out_row(const CachedAttention& a, const StateT
 // ---- sharing the work ----
 // The blocks of 32 slots of all (state, k/v head) pairs, in that order, are one list; workgroup w takes the entries
 // w share .. (w + 1) share - 1.  States of different length so cost every workgroup the same.
-__device__ __forceinline__ int state_blocks(const CachedAttention& a, int b) {
-    const StateTokens st = state_tokens(a.t, a.c, b);
-    return st.n ? (st.len + 31) >> 5 : 0;
-}
+__device__ __forceinline__ int blocks_of(const StateTokens& st) { return st.n ? (st.len + 31) >> 5 : 0; }
+__device__ __forceinline__ int state_blocks(const CachedAttention& a, int b) { return blocks_of(state_tokens(a.t, a.c, b)); }
 // Per wavefront: blocks of the states in front of this lane's stretch of states, and of all.
 struct Prefix {
     int stretch;              // states per lane
     int before, total;
+    StateTokens own;          // the last of this lane's states (where there are at most 64: state `lane`)
 };
 __device__ __forceinline__ Prefix prefix_blocks(const CachedAttention& a, int lane) {
     Prefix p;
     p.stretch = (a.t.B + 63) / 64;
     int mine = 0;
-    for (int b = lane * p.stretch; b < (lane + 1) * p.stretch && b < a.t.B; ++b) mine += state_blocks(a, b);
+    p.own = StateTokens{0, 0, 0, 0};
+    for (int b = lane * p.stretch; b < (lane + 1) * p.stretch && b < a.t.B; ++b) {
+        p.own = state_tokens(a.t, a.c, b);
+        mine += blocks_of(p.own);
+    }
     int x = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -419,96 +424,146 @@ __device__ __forceinline__ unsigned share_of(const Plan& p, unsigned entries) { 
 // Nothing is shared between wavefronts but the query rows: keys go from memory into operand registers, values through a region of
 // LDS of the wavefront's own, where the transposing reads turn them.  The next block's keys are requested as soon as the scores
 // have been taken, its values as soon as this block's have been stored, so that loads are in flight all the time.
+// A workgroup may have to finish one (state, k/v head) and go on with the next: the wavefronts' first blocks of the next segment are
+// requested like any next block, so that the end of a segment (6 us: sums joined, queries of the next read) has loads in flight.
+template <int DT, int DH>
+struct StreamShape {
+    typedef Shape<DT, DH> S;
+    static constexpr int OS = S::ROW + 4;                              // floats of a row of O in LDS: rows start on different banks
+    static constexpr int LDS = S::LDS > 16 * OS * 4 ? S::LDS : 16 * OS * 4;
+};
+
 template <int DT, int DH>
 __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a, Plan p) {
     typedef Shape<DT, DH> S;
+    constexpr int OS = StreamShape<DT, DH>::OS, LDS = StreamShape<DT, DH>::LDS;
     extern __shared__ __attribute__((aligned(16))) char lds_all[];
     __shared__ uint4 s_q[S::KS * 2 * 64];                              // query fragments: [step][hi, lo][64 lanes]
-    __shared__ float2 s_ml[8][16];
+    __shared__ float2 s_ml[8][16];                                     // per wavefront and row: reference and sum
+    __shared__ float s_l[8][16];                                       // sums relative to the largest reference
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int c = lane & 15, g = lane >> 4;
-    char* lds = lds_all + wave * S::LDS;
+    char* lds = lds_all + wave * LDS;
 
     // this workgroup's entries: left of them, the state and head they begin in, the block in it
-    int b, h, block, left;
+    int b, h, first, left;
+    StateTokens st;
+    Prefix pre;
+    pre.stretch = 0;
+    auto tokens_of = [&](int x) {                                      // of state x
+        StateTokens t;
+        if (pre.stretch == 1) {
+            t.row0 = lane_value(pre.own.row0, x);
+            t.n = lane_value(pre.own.n, x);
+            t.len = lane_value(pre.own.len, x);
+            t.base = lane_value(pre.own.base, x);
+        } else {
+            t = state_tokens(a.t, a.c, x);
+        }
+        return t;
+    };
     if (p.groups == 0) {
-        h = blockIdx.x % a.c.n_kv; b = blockIdx.x / a.c.n_kv; block = 0;
+        h = blockIdx.x % a.c.n_kv; b = blockIdx.x / a.c.n_kv; first = 0;
         left = 0x7fffffff;
+        st = tokens_of(b);
     } else {
-        const Prefix pre = prefix_blocks(a, lane);
+        pre = prefix_blocks(a, lane);
         const unsigned entries = (unsigned)pre.total * a.c.n_kv, share = share_of(p, entries);
-        if (blockIdx.x > (entries - 1) / share || entries == 0) return;
+        if (entries == 0 || blockIdx.x > (entries - 1) / share) return;
         unsigned at = blockIdx.x * share;
         left = (int)(entries - at < share ? entries - at : share);
         const unsigned long long in = __ballot((unsigned)pre.before * a.c.n_kv <= at);
         const int l = 63 - __builtin_clzll(in);                         // the last stretch that begins at or before the entry
         at -= (unsigned)lane_value(pre.before, l) * a.c.n_kv;
         b = l * pre.stretch;
-        unsigned n = state_blocks(a, b);
+        st = tokens_of(b);
+        unsigned n = blocks_of(st);
         while (at >= n * a.c.n_kv) {
             at -= n * a.c.n_kv;
-            n = state_blocks(a, ++b);
+            st = tokens_of(++b);
+            n = blocks_of(st);
         }
         h = at / n;
-        block = at % n;
+        first = at % n;
     }
+    if (st.n == 0) return;                                             // (one workgroup per (state, k/v head), nothing new)
+    auto next_segment = [&](int& x, int& y, StateTokens& t) {          // (there is one: entries are left)
+        if (++y < a.c.n_kv) return;
+        y = 0;
+        do t = tokens_of(++x);
+        while (blocks_of(t) == 0);
+    };
+    int blocks = blocks_of(st);
+    int last = left < blocks - first ? first + left : blocks;
+
+    KeyLoads<S> keys;
+    ValueLoads<S> values;
+    float4 ks[2], vs[2];                                               // int8: scales of this lane's keys
+    auto scales = [&](const float* pool, int x_lo, int x_hi, float4 (&f)[2]) {
+        f[0] = *reinterpret_cast<const float4*>(pool + (x_lo < 0 ? 0 : x_lo) + (unsigned)(4 * g));
+        f[1] = *reinterpret_cast<const float4*>(pool + (x_hi < 0 ? 0 : x_hi) + (unsigned)(4 * g));
+    };
+    int page_lo = -1, page_hi = -1;                                    // rows of the lane-th block ahead
+    auto pages = [&](int t0) {
+        const int block = t0 + lane * waves, slot = block * 32;
+        page_lo = block < last && slot < st.len ? kv_row_index(a.c, b, h, slot) : -1;
+        page_hi = block < last && slot + 16 < st.len ? kv_row_index(a.c, b, h, slot + 16) : -1;
+    };
+    constexpr int JOBS = S::KS * 64;                                   // query fragments: a lane of a step each, of the first threads
+    static_assert(JOBS <= 256, "every workgroup has the threads");
+    const int d0 = 32 * wave + 8 * g;
+    auto query_row = [&]() { return c < st.n * p.group ? c : st.n * p.group - 1; };
+    auto position = [&]() { return rope_position(a.t, st.row0 + query_row() / p.group, st.base + query_row() / p.group); };
+    int pos = position();
+    pages(first + wave);
+    int lo = lane_value(page_lo, 0), hi = lane_value(page_hi, 0);      // where the block under way lies
+    keys.request(a.c.k, lo, hi, lane);
+    if constexpr (DT == BRL_I8) scales(a.c.ks, lo, hi, ks);
+    values.request(a.c.v, lo, hi, lane);
+    if constexpr (DT == BRL_I8) scales(a.c.vs, lo, hi, vs);
     bool before = true;                                                // nothing but this segment's beginning lies in front
     for (;;) {
-        const StateTokens st = state_tokens(a.t, a.c, b);
         const int rows = st.n * p.group, seen = st.len;                // (the last token sees them all, or bits of the mask)
-        const int blocks = rows ? (seen + 31) >> 5 : 0;
-        const int first = block, last = left < blocks - block ? block + left : blocks;
-        if (rows) {
-        const bool all = first == 0 && last == blocks;
+        const bool all = first == 0 && last == blocks, live = c < rows;
+        const int token = query_row() / p.group;
         QueryPart<S> q;
-        constexpr int JOBS = S::KS * 64;                               // a lane of a step's fragment each, of the first threads
-        static_assert(JOBS <= 256, "every workgroup has the threads");
-        const bool live = c < rows;
-        const int d0 = 32 * wave + 8 * g;
         if (threadIdx.x < JOBS) {
-            const QueryRow from(a, st, h, p.group, live ? c : rows - 1);
+            const QueryRow from(a, st, h, p.group, query_row(), pos);
             q.request(from.x, from.ct, from.sn, d0);
         }
-        RowState<S> row;
-        float unit = 0x1p126f;                                         // int8: power of two that the sums are multiplied by
-        row.clear();
-        const int token = (live ? c : rows - 1) / p.group;
-        const int all_see = st.base + (a.tree ? 0 : 1);                // slots below are seen by every row (causal: by token 0)
-
-        int page_lo = -1, page_hi = -1;                                // rows of the lane-th block ahead
-        auto pages = [&](int t0) {
-            const int slot = (t0 + lane * waves) * 32;
-            page_lo = slot < seen ? kv_row_index(a.c, b, h, slot) : -1;
-            page_hi = slot + 16 < seen ? kv_row_index(a.c, b, h, slot + 16) : -1;
-        };
-        KeyLoads<S> keys;
-        ValueLoads<S> values;
-        int lo = -1, hi = -1;                                          // where the current block lies
-        float4 ks[2], vs[2];                                           // int8: scales of this lane's keys
-        auto scales = [&](const float* pool, int x_lo, int x_hi, float4 (&f)[2]) {
-            f[0] = *reinterpret_cast<const float4*>(pool + (x_lo < 0 ? 0 : x_lo) + (unsigned)(4 * g));
-            f[1] = *reinterpret_cast<const float4*>(pool + (x_hi < 0 ? 0 : x_hi) + (unsigned)(4 * g));
-        };
-        int t = first + wave, ahead = 0;
-        if (t < last) {
-            pages(t);
-            lo = lane_value(page_lo, 0);
-            hi = lane_value(page_hi, 0);
-            keys.request(a.c.k, lo, hi, lane);
-            if constexpr (DT == BRL_I8) scales(a.c.ks, lo, hi, ks);
-            values.request(a.c.v, lo, hi, lane);
-            if constexpr (DT == BRL_I8) scales(a.c.vs, lo, hi, vs);
+        // where this wavefront's first block of the next segment lies
+        left -= last - first;
+        if (p.groups == 0) left = 0;
+        int after_lo = -1, after_hi = -1;
+        if (left > 0) {
+            int x = b, y = h;
+            StateTokens next = st;
+            next_segment(x, y, next);
+            const int n = blocks_of(next), slot = wave * 32;
+            if (wave < (left < n ? left : n)) {
+                after_lo = kv_row_index(a.c, x, y, slot);
+                after_hi = slot + 16 < next.len ? kv_row_index(a.c, x, y, slot + 16) : -1;
+            }
         }
+        RowState<S> row;
+        row.clear();
+        float unit = 0x1p126f;                                         // int8: power of two that the sums are multiplied by
+        const int all_see = st.base + (a.tree ? 0 : 1);                // slots below are seen by every row (causal: by token 0)
         if (threadIdx.x < JOBS) {
             uint4 x, y;
             q.split(live, d0, x, y);
             s_q[2 * wave * 64 + lane] = x;
             s_q[(2 * wave + 1) * 64 + lane] = y;
         }
+        after_lo = __builtin_amdgcn_readfirstlane(after_lo);
+        after_hi = __builtin_amdgcn_readfirstlane(after_hi);
         __syncthreads();
-        for (; t < last; t += waves) {
+        int t = first + wave, ahead = 0;
+        // A wavefront without a block takes a turn, too: for the requests, nothing else.  (A branch around it costs the loop registers.)
+        const bool mine = t < last;
+        do {
             const int slot0 = t * 32;
-            int at = lane;                                             // (opaque: or the compiler keeps all of LDS in registers)
+            unsigned at = lane;                                        // (opaque: or the compiler keeps all of LDS in registers)
             asm volatile("" : "+v"(at));
             float s[8];
             block_scores<S>(keys, s_q, at, s);
@@ -518,18 +573,18 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
                 for (int e = 0; e < 8; ++e) s[e] *= f[e];
             }
             __builtin_amdgcn_sched_barrier(0);                         // (the old keys' registers are free from here on)
-            // Behind the last block, rows 0 of the pool are requested and never used: a request that might not be made would
+            // Behind the very last block, rows 0 of the pool are requested and never used: a request that might not be made would
             // have every wait in the loop wait for all of them.
             if (++ahead == 64) {
                 ahead = 0;
                 pages(t + waves);
             }
             const bool more = t + waves < last;
-            const int next_lo = more ? lane_value(page_lo, ahead) : -1, next_hi = more ? lane_value(page_hi, ahead) : -1;
+            const int next_lo = more ? lane_value(page_lo, ahead) : after_lo, next_hi = more ? lane_value(page_hi, ahead) : after_hi;
             keys.request(a.c.k, next_lo, next_hi, lane);
             if constexpr (DT == BRL_I8) scales(a.c.ks, next_lo, next_hi, ks);
             __builtin_amdgcn_sched_barrier(0);
-            const bool whole = slot0 + 32 <= all_see && lo >= 0 && hi >= 0;
+            const bool whole = slot0 + 32 <= all_see && mine && lo >= 0 && hi >= 0;
             float vf[8];
             if constexpr (DT == BRL_I8) {
                 const float f[8] = {vs[0].x, vs[0].y, vs[0].z, vs[0].w, vs[1].x, vs[1].y, vs[1].z, vs[1].w};
@@ -538,17 +593,17 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
             }
             values.store(lds, at);
             if (!whole) {
-                const int n = seen - slot0;
-                uint32_t there = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+                const int n = mine ? seen - slot0 : 0;
+                uint32_t there = n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1u : 0u;
                 if (lo < 0) there &= 0xffff0000u;
                 if (hi < 0) there &= 0x0000ffffu;
                 if (there != 0xffffffffu) clear_rows<S>(lds, lane, there);
-                const uint32_t mine = bits_of_group(there, g);
+                const uint32_t own = bits_of_group(there, g);
                 if constexpr (DT == BRL_I8) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) vf[e] = mine >> e & 1u ? vf[e] : 0.f;
+                    for (int e = 0; e < 8; ++e) vf[e] = own >> e & 1u ? vf[e] : 0.f;
                 }
-                const uint32_t bits = mine & bits_of_group(visible_bits(a, st, token, slot0), g);
+                const uint32_t bits = own & bits_of_group(visible_bits(a, st, token, slot0), g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s[e] = bits >> e & 1u ? s[e] : -INFINITY;
             }
@@ -556,6 +611,9 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
             values.request(a.c.v, next_lo, next_hi, lane);
             if constexpr (DT == BRL_I8) scales(a.c.vs, next_lo, next_hi, vs);
             __builtin_amdgcn_sched_barrier(0);
+            lo = next_lo;
+            hi = next_hi;
+            if (!mine) break;
             if (p.scores && live) {
                 float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_pad + c) * p.ld_scores + slot0 + 4 * g;
                 reinterpret_cast<float4*>(f)[0] = make_float4(s[0], s[1], s[2], s[3]);
@@ -579,33 +637,34 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
             __builtin_amdgcn_wave_barrier();
             block_values<S, 1>(lds, &s, &row, at);
             __builtin_amdgcn_wave_barrier();
-            lo = next_lo;
-            hi = next_hi;
-        }
+            t += waves;
+        } while (t < last);
         // the wavefronts' parts meet: sums to the largest reference, then O over LDS
         row.l += __shfl_xor(row.l, 16, 64);
         row.l += __shfl_xor(row.l, 32, 64);
         if (g == 0) s_ml[wave][c] = make_float2(row.l > 0.f ? row.ref : -INFINITY, row.l);
         __syncthreads();
         float top = -INFINITY;
+#pragma unroll 4
         for (int w = 0; w < waves; ++w) top = fmaxf(top, s_ml[w][c].x);
         float f = row.l > 0.f ? __builtin_amdgcn_exp2f(row.ref - top) : 0.f;
+        if (g == 0) s_l[wave][c] = row.l * f;
         if constexpr (DT == BRL_I8) f /= unit;
-        float* o = reinterpret_cast<float*>(lds);                      // [16 rows][ROW]
+        float* o = reinterpret_cast<float*>(lds);                      // [16 rows][OS]
 #pragma unroll
-        for (int d = 0; d < S::DTL; ++d) *reinterpret_cast<v4f*>(o + c * S::ROW + 16 * d + 4 * g) = row.o[d] * f;
+        for (int d = 0; d < S::DTL; ++d) *reinterpret_cast<v4f*>(o + c * OS + 16 * d + 4 * g) = row.o[d] * f;
         __syncthreads();
         const size_t slot = (2 * (size_t)blockIdx.x + (before ? 0 : 1)) * p.rows_pad;
-        for (int i = threadIdx.x; i < 16 * S::ROW / 4; i += blockDim.x) {
+        for (int i = threadIdx.x; i < rows * (S::ROW / 4); i += blockDim.x) {
             const int r = i / (S::ROW / 4), d = i % (S::ROW / 4) * 4;
-            if (r >= rows || d >= DH) continue;
+            if (d >= DH) continue;
             float ref = -INFINITY, l = 0.f;
-            for (int w = 0; w < waves; ++w) ref = fmaxf(ref, s_ml[w][r].x);
             v4f sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
             for (int w = 0; w < waves; ++w) {
-                const float2 ml = s_ml[w][r];
-                if (ml.y > 0.f) l += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
-                sum += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds_all + w * S::LDS) + r * S::ROW + d);
+                ref = fmaxf(ref, s_ml[w][r].x);
+                l += s_l[w][r];
+                sum += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds_all + w * LDS) + r * OS + d);
             }
             if (all) {
                 *reinterpret_cast<v4f*>(out_row(a, st, h, p.group, r) + d) = sum * (l > 0.f ? 1.f / l : 0.f);
@@ -615,17 +674,15 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
                 if (d == 0) p.part_ml[slot + r] = make_float2(ref, l);
             }
         }
-        __syncthreads();
-        }
-        if (p.groups == 0) return;
-        left -= last - first;
         if (left <= 0) return;
+        __syncthreads();
         before = false;
-        block = 0;
-        if (++h == a.c.n_kv || blocks == 0) {
-            h = 0;
-            ++b;
-        }
+        next_segment(b, h, st);
+        blocks = blocks_of(st);
+        first = 0;
+        last = left < blocks ? left : blocks;
+        pages(wave);
+        pos = position();
     }
 }
 
@@ -745,14 +802,14 @@ struct SharedLoads {
     static constexpr int N = (32 * S::CPR + 255) / 256;
     uint4 k[N], v[N];
     float scale;
-    __device__ __forceinline__ void request(const KvView& c, int lo, int hi, int tid) {
+    __device__ __forceinline__ void request(const KvView& c, int lo, int hi, unsigned tid) {
         const size_t lo_at = (size_t)(lo < 0 ? 0 : lo) * S::RB, hi_at = (size_t)(hi < 0 ? 0 : hi) * S::RB;
         constexpr int HALF = 16 * S::CPR;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            int idx = i * 256 + tid;                                   // (past the end: the last chunk again, see ValueLoads)
-            if (N * 256 > 32 * S::CPR && idx >= 32 * S::CPR) idx = 32 * S::CPR - 1;
-            const size_t at = idx >= HALF ? hi_at + (size_t)((idx - HALF) * 16) : lo_at + (size_t)(idx * 16);
+            unsigned idx = i * 256 + tid;                              // (past the end: the last chunk again, see ValueLoads)
+            if (N * 256 > 32 * S::CPR && idx >= 32u * S::CPR) idx = 32 * S::CPR - 1;
+            const size_t at = idx >= (unsigned)HALF ? hi_at + (size_t)((idx - HALF) * 16) : lo_at + (size_t)(idx * 16);
             k[i] = *reinterpret_cast<const uint4*>(c.k + at);
             v[i] = *reinterpret_cast<const uint4*>(c.v + at);
         }
@@ -762,16 +819,16 @@ struct SharedLoads {
         }
     }
     // there: bit per key whose row holds numbers
-    __device__ __forceinline__ void store(char* lds, float* scales, int tid, uint32_t there) {
+    __device__ __forceinline__ void store(char* lds, float* scales, unsigned tid, uint32_t there) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int idx = i * 256 + tid, key = idx / S::CPR, ch = idx % S::CPR;
-            if (N * 256 > 32 * S::CPR && idx >= 32 * S::CPR) continue;
+            const unsigned idx = i * 256 + tid, key = idx / S::CPR, ch = idx % S::CPR;
+            if (N * 256 > 32 * S::CPR && idx >= 32u * S::CPR) continue;
             uint4 x = k[i], y = v[i];
             if (there != 0xffffffffu && !(there >> key & 1u)) y = make_uint4(0, 0, 0, 0);
             if constexpr (S::ROW > S::DH) {                            // what lies behind head_dim is not a number
                 constexpr int PER = 16 / S::SZ;
-                const int valid = S::DH - ch * PER;                    // elements of this chunk
+                const int valid = S::DH - (int)ch * PER;                    // elements of this chunk
                 uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[j] = j * (4 / S::SZ) < valid ? w[j] : 0u;
@@ -784,7 +841,7 @@ struct SharedLoads {
             if (tid < 64) scales[tid] = there >> (tid & 31) & 1u ? scale : 0.f;
         }
     }
-    static __device__ __forceinline__ void put(char* lds, int key, int ch, const uint4& r) {
+    static __device__ __forceinline__ void put(char* lds, unsigned key, unsigned ch, const uint4& r) {
         if constexpr (S::DT == BRL_F16) {
             *reinterpret_cast<uint4*>(lds + lds_chunk<S>(key, ch)) = r;
         } else if constexpr (S::DT == BRL_F32) {
@@ -1159,7 +1216,7 @@ template <int DT, int DH>
 int launch_few(const CachedAttention& a, const Layout& L, hipStream_t s) {
     const Plan& p = L.p;
     const dim3 grid((unsigned)(p.groups ? p.groups : a.t.B * a.c.n_kv)), block(L.waves * 64);
-    const size_t lds = (size_t)L.waves * Shape<DT, DH>::LDS;
+    const size_t lds = (size_t)L.waves * StreamShape<DT, DH>::LDS;
     hipLaunchKernelGGL((cached_stream_kernel<DT, DH>), grid, block, lds, s, a, p);
     BRL_LAUNCH_CHECK("cached_stream_kernel");
     if (p.groups) {
