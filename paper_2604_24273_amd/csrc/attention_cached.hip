@@ -11,6 +11,7 @@
 // 4 g + 3 of both tiles.  The contraction of the second product may run over the keys in any order: with those eight as the
 // slots that lane has to fill of operand P, the probabilities never leave their lane.
 #include <cstring>
+#include <type_traits>
 
 #include "common.hpp"
 
@@ -61,7 +62,13 @@ struct Shape {
     static constexpr int LS = NCH * 16, PLANE = 32 * LS;               // bytes of such a row, of a block's plane
     static constexpr int LDS = PL * PLANE;
     static constexpr int NV = (32 * CPR + 63) / 64;                    // loads of a wavefront for a block of rows
-    static constexpr int KL = DT == BRL_F32 ? 2 : 1;                   // 16-byte (int8: 8-byte) loads of a key fragment
+    // Key fragments straight from memory: which components a lane of group g holds in step s is free as long as the queries go along.
+    // Chosen such that four lanes read 64 bytes of a row with each load: 32 s + 8 g .. + 7 of fp16 rows; 32 s + 4 g .. + 3 and sixteen
+    // further on of fp32 rows (two loads a step); of int8 rows 64 u + 16 g .. + 15 with one load for the steps 2 u and 2 u + 1 (8 bytes
+    // a lane where a row is shorter than that).
+    static constexpr bool PAIRED = DT == BRL_I8 && ROW > 32;
+    static constexpr int KL = DT == BRL_F32 ? 2 * KS : PAIRED ? KS / 2 : KS;      // loads of a tile
+    static_assert(!PAIRED || KS % 2 == 0, "whole pairs of steps");
 };
 
 // Where chunk c of a key's row lies in LDS.  The chunks of a row are permuted by bits of the key such that both the 16 rows
@@ -75,60 +82,88 @@ __device__ __forceinline__ unsigned lds_chunk(unsigned key, unsigned c) {      /
 // A block of 32 slots lies in two halves of 16 (pages hold 16 at least): lo and hi are their first rows in the pool, -1 where
 // there is none.
 
-template <int DT>
-struct Raw { typedef uint4 type; };
-template <>
-struct Raw<BRL_I8> { typedef uint2 type; };
-
-// Fragments of the keys straight from the pool: lane 16 g + c reads, of the key in row c of each tile, components 32 s + 8 g on.
+// The keys of a block, lane 16 g + c those of row c of both tiles.
 template <class S>
 struct KeyLoads {
-    typename Raw<S::DT>::type raw[2][S::KS][S::KL];
-    __device__ __forceinline__ void request(const char* pool, int lo, int hi, int lane) {
-        const int c = lane & 15, g = lane >> 4;
+    static constexpr bool WIDE = S::DT != BRL_I8 || S::PAIRED;         // 16 bytes a lane, else 8
+    static constexpr int STEP = WIDE ? 64 : 32;                        // bytes of a row that a load covers
+    typedef typename std::conditional<WIDE, uint4, uint2>::type raw_t;
+    raw_t raw[2][S::KL];
+    __device__ __forceinline__ void request(const char* pool, int lo, int hi, unsigned lane) {
+        const unsigned c = lane & 15, g = lane >> 4, mine = g * (STEP / 4);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int row = t ? hi : lo;
             const char* p = pool + (size_t)(row < 0 ? 0 : row) * S::RB;          // (the same for all lanes)
 #pragma unroll
-            for (int s = 0; s < S::KS; ++s) {
-                unsigned at = (unsigned)(c * S::RB + 8 * g * S::SZ);
-                if (S::KS * 32 > S::ROW && s == S::KS - 1 && 32 * s + 8 * g + 8 > S::ROW) at = (unsigned)(c * S::RB);   // (a row ends inside the step)
-                else at += (unsigned)(s * 32 * S::SZ);
-#pragma unroll
-                for (int i = 0; i < S::KL; ++i)
-                    raw[t][s][i] = *reinterpret_cast<const typename Raw<S::DT>::type*>(p + (at + (unsigned)(i * 16)));
+            for (int i = 0; i < S::KL; ++i) {
+                unsigned at = c * S::RB;                               // (past the end of a row: its beginning, not used)
+                if ((i + 1) * STEP <= S::RB || i * STEP + mine < (unsigned)S::RB) at += i * STEP + mine;
+                raw[t][i] = *reinterpret_cast<const raw_t*>(p + at);
             }
         }
     }
+    // the operand of step s
     __device__ __forceinline__ void fragment(int t, int s, unsigned lane, v8h (&f)[S::PL]) const {
         uint32_t w[S::PL][4];
+        const int g = (int)(lane >> 4);
+        int first, second;                                             // components of the first and the second four
         if constexpr (S::DT == BRL_F32) {
+            first = 32 * s + 4 * g;
+            second = first + 16;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint4 r = raw[t][s][i];
+                const uint4 r = raw[t][2 * s + i];
                 split_pair(__uint_as_float(r.x), __uint_as_float(r.y), w[0][2 * i], w[1][2 * i]);
                 split_pair(__uint_as_float(r.z), __uint_as_float(r.w), w[0][2 * i + 1], w[1][2 * i + 1]);
             }
         } else if constexpr (S::DT == BRL_F16) {
-            const uint4 r = raw[t][s][0];
+            first = 32 * s + 8 * g;
+            second = first + 4;
+            const uint4 r = raw[t][s];
             w[0][0] = r.x; w[0][1] = r.y; w[0][2] = r.z; w[0][3] = r.w;
+        } else if constexpr (S::PAIRED) {
+            first = 64 * (s / 2) + 16 * g + 8 * (s % 2);
+            second = first + 4;
+            const uint4 r = raw[t][s / 2];
+            widen_codes(s % 2 ? r.z : r.x, w[0][0], w[0][1]);
+            widen_codes(s % 2 ? r.w : r.y, w[0][2], w[0][3]);
         } else {
-            const uint2 r = raw[t][s][0];
-            widen_codes(r.x, w[0][0], w[0][1]);
-            widen_codes(r.y, w[0][2], w[0][3]);
+            first = 32 * s + 8 * g;
+            second = first + 4;
+            widen_codes(raw[t][s].x, w[0][0], w[0][1]);
+            widen_codes(raw[t][s].y, w[0][2], w[0][3]);
         }
-        if (S::KS * 32 > S::DH && s == S::KS - 1) {                    // what lies behind head_dim is not a number
-            const int valid = S::DH - (32 * s + 8 * (int)(lane >> 4));
+        // what lies behind head_dim is not a number (four components are on one side of it or the other)
+        static_assert(S::DH % 4 == 0, "whole fours");
+        if (S::DH % (S::PAIRED ? 64 : 32) && s >= S::KS - (S::PAIRED ? 2 : 1)) {
 #pragma unroll
             for (int p = 0; p < S::PL; ++p)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[p][j] = 2 * j < valid ? w[p][j] : 0u;
+                for (int j = 0; j < 4; ++j) w[p][j] = (j < 2 ? first : second) < S::DH ? w[p][j] : 0u;
         }
 #pragma unroll
         for (int p = 0; p < S::PL; ++p) f[p] = __builtin_bit_cast(v8h, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
     }
 };
+// Components 32 s + 8 g .. + 7 of the rows of a query tile (lane 16 g + c has them of row c) to where the operand of KeyLoads' fragments
+// wants them, in [step][hi, lo][64 lanes].
+template <class S>
+__device__ __forceinline__ void store_query(uint4* to, int s, int lane, const uint4& hi, const uint4& lo) {
+    const int c = lane & 15, g = lane >> 4;
+    if constexpr (S::DT == BRL_F32) {
+        uint2* f = reinterpret_cast<uint2*>(to) + (s * 2 * 64 + 16 * (2 * (g & 1)) + c) * 2 + (g >> 1);
+        f[0] = make_uint2(hi.x, hi.y);
+        f[32] = make_uint2(hi.z, hi.w);                                // sixteen lanes on
+        f[128] = make_uint2(lo.x, lo.y);
+        f[160] = make_uint2(lo.z, lo.w);
+    } else {
+        const int n = 4 * s + g;                                       // which eight components of the row
+        const int step = S::PAIRED ? 2 * (n >> 3) + (n & 1) : s, group = S::PAIRED ? (n & 7) >> 1 : g;
+        to[step * 128 + 16 * group + c] = hi;
+        to[step * 128 + 64 + 16 * group + c] = lo;
+    }
+}
 
 // Rows of the values, 16 bytes per lane in the order of the pool, and from there as halfs into LDS.
 template <class S>
@@ -552,8 +587,7 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         if (threadIdx.x < JOBS) {
             uint4 x, y;
             q.split(live, d0, x, y);
-            s_q[2 * wave * 64 + lane] = x;
-            s_q[(2 * wave + 1) * 64 + lane] = y;
+            store_query<S>(s_q, wave, lane, x, y);
         }
         after_lo = __builtin_amdgcn_readfirstlane(after_lo);
         after_hi = __builtin_amdgcn_readfirstlane(after_hi);
@@ -933,11 +967,8 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
             q.split(rr < rows, 32 * s + 8 * g, x, y);
             qh[r][s] = __builtin_bit_cast(v8h, x);
             ql[r][s] = __builtin_bit_cast(v8h, y);
-            if (p.q && split == 0 && w0 + r * 16 <= r1) {
-                uint4* f = p.q + ((((size_t)unit * p.rows_pad + w0 + r * 16) / 16 * S::KS + s) * 2) * 64 + lane;
-                f[0] = x;
-                f[64] = y;
-            }
+            if (p.q && split == 0 && w0 + r * 16 <= r1)
+                store_query<S>(p.q + ((size_t)unit * p.rows_pad + w0 + r * 16) / 16 * S::KS * 128, s, lane, x, y);
         }
     }
     if constexpr (S::NCH * 8 > S::ROW) {                               // components of the last step that no row has
