@@ -1006,7 +1006,8 @@ int check_new_tokens(const KvView& v, const float* qkv, int n_heads, int T, int 
     BRL_REQUIRE(rope_len >= 1, "%s: rope_len = %d", who, rope_len);
     if (max_new > T) max_new = T;
     // workgroups and items of a launch are counted in 32 bits
-    BRL_REQUIRE((long long)max_new * n_heads * B <= (1ll << 26) && (long long)B * n_heads <= (1 << 22),
+    BRL_REQUIRE((long long)max_new * n_heads * B <= (1ll << 26) && (long long)B * n_heads <= (1 << 22) &&
+                    (long long)max_new * (n_heads / v.n_kv) * (n_heads / v.n_kv) < (1ll << 32),
                 "%s: too much for one call (max_new %d, B %d, n_heads %d)", who, max_new, B, n_heads);
     t.cu = cu_new; t.lens = lens; t.pos = positions;
     t.cos_t = rope_cos; t.sin_t = rope_sin;

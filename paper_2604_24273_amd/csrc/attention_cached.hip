@@ -245,13 +245,19 @@ struct ValueReads {
     }
 };
 
+// Query heads per k/v head.  Rows are divided by them often enough to multiply by the inverse instead: ceil(2^32 / n), right for
+// rows below 2^32 / n, which the entry point sees to; 0 stands for one head.
+struct Group {
+    int n;
+    uint32_t inverse;
+    __device__ __forceinline__ int token(int r) const { return inverse ? (int)__umulhi((uint32_t)r, inverse) : r; }
+};
+
 struct QueryRow {
     const float *x, *ct, *sn;          // a query row, the cosines and sines of its position
-    __device__ __forceinline__ QueryRow(const CachedAttention& a, const StateTokens& st, int h, int group, int r)
-        : QueryRow(a, st, h, group, r, rope_position(a.t, st.row0 + r / group, st.base + r / group)) {}
-    __device__ __forceinline__ QueryRow(const CachedAttention& a, const StateTokens& st, int h, int group, int r, int pos) {
-        const int i = r / group, row = st.row0 + i, dh = a.c.dh;
-        x = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * dh) + (h * group + r % group) * dh;
+    __device__ __forceinline__ QueryRow(const CachedAttention& a, const StateTokens& st, int h, const Group& group, int r, int token, int pos) {
+        const int row = st.row0 + token, dh = a.c.dh;
+        x = a.qkv + (size_t)row * ((a.n_heads + 2 * a.c.n_kv) * dh) + (h * group.n + r - token * group.n) * dh;
         ct = a.t.cos_t + (size_t)pos * (dh / 2);
         sn = a.t.sin_t + (size_t)pos * (dh / 2);
     }
@@ -403,7 +409,8 @@ __device__ __forceinline__ void block_values(const char* lds, const float (*p)[8
 }
 
 struct Plan {
-    int group, rows_max;      // query heads per k/v head; rows of a state at most
+    Group group;
+    int rows_max;             // rows of a state at most
     int row_blocks, splits;   // many rows: blocks of rows of a (state, k/v head), parts of the keys
     uint4* q;                 // many rows with weights: [B][n_kv][rows_pad / 16][steps][hi, lo][64] query fragments
     int rows_pad;             // rows reserved per (state, k/v head) in the scratch space
@@ -416,8 +423,9 @@ struct Plan {
     size_t ld_scores;
 };
 
-__device__ __forceinline__ float* out_row(const CachedAttention& a, const StateTokens& st, int h, int group, int r) {
-    return a.out + ((size_t)(st.row0 + r / group) * a.n_heads + h * group + r % group) * a.c.dh;
+__device__ __forceinline__ float* out_row(const CachedAttention& a, const StateTokens& st, int h, const Group& group, int r) {
+    const int token = group.token(r);
+    return a.out + ((size_t)(st.row0 + token) * a.n_heads + h * group.n + r - token * group.n) * a.c.dh;
 }
 
 // ---- sharing the work ----
@@ -547,9 +555,9 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
     constexpr int JOBS = S::KS * 64;                                   // query fragments: a lane of a step each, of the first threads
     static_assert(JOBS <= 256, "every workgroup has the threads");
     const int d0 = 32 * wave + 8 * g;
-    auto query_row = [&]() { return c < st.n * p.group ? c : st.n * p.group - 1; };
-    auto position = [&]() { return rope_position(a.t, st.row0 + query_row() / p.group, st.base + query_row() / p.group); };
-    int pos = position();
+    auto query_row = [&]() { return c < st.n * p.group.n ? c : st.n * p.group.n - 1; };
+    auto position = [&](int token) { return rope_position(a.t, st.row0 + token, st.base + token); };
+    int token = p.group.token(query_row()), pos = position(token);
     pages(first + wave);
     int lo = lane_value(page_lo, 0), hi = lane_value(page_hi, 0);      // where the block under way lies
     keys.request(a.c.k, lo, hi, lane);
@@ -558,12 +566,11 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
     if constexpr (DT == BRL_I8) scales(a.c.vs, lo, hi, vs);
     bool before = true;                                                // nothing but this segment's beginning lies in front
     for (;;) {
-        const int rows = st.n * p.group, seen = st.len;                // (the last token sees them all, or bits of the mask)
+        const int rows = st.n * p.group.n, seen = st.len;                // (the last token sees them all, or bits of the mask)
         const bool all = first == 0 && last == blocks, live = c < rows;
-        const int token = query_row() / p.group;
         QueryPart<S> q;
         if (threadIdx.x < JOBS) {
-            const QueryRow from(a, st, h, p.group, query_row(), pos);
+            const QueryRow from(a, st, h, p.group, query_row(), token, pos);
             q.request(from.x, from.ct, from.sn, d0);
         }
         // where this wavefront's first block of the next segment lies
@@ -716,7 +723,8 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         first = 0;
         last = left < blocks ? left : blocks;
         pages(wave);
-        pos = position();
+        token = p.group.token(query_row());
+        pos = position(token);
     }
 }
 
@@ -773,7 +781,7 @@ template <int DH>
 __global__ __launch_bounds__(256) void cached_join_kernel(CachedAttention a, Plan p) {
     const int r = blockIdx.x % p.rows_max, h = blockIdx.x / p.rows_max % a.c.n_kv, b = blockIdx.x / p.rows_max / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
-    if (r >= st.n * p.group) return;
+    if (r >= st.n * p.group.n) return;
     const int lane = threadIdx.x & 63;
     const Prefix pre = prefix_blocks(a, lane);
     const unsigned share = share_of(p, (unsigned)pre.total * a.c.n_kv);
@@ -800,7 +808,7 @@ __global__ __launch_bounds__(256) void cached_join_splits_kernel(CachedAttention
     const int r = (int)(i % p.rows_max), unit = (int)(i / p.rows_max), h = unit % a.c.n_kv, b = unit / a.c.n_kv;
     if (b >= a.t.B) return;
     const StateTokens st = state_tokens(a.t, a.c, b);
-    if (r >= st.n * p.group) return;
+    if (r >= st.n * p.group.n) return;
     const size_t at = ((size_t)unit * p.rows_pad + r) * p.splits;
     Joiner<DH, GROUPS>::run(p, 0u, (unsigned)p.splits - 1, [&](unsigned w) { return at + w; }, out_row(a, st, h, p.group, r),
                             p.lse ? p.lse + (size_t)unit * p.rows_pad + r : nullptr);
@@ -810,7 +818,7 @@ __global__ __launch_bounds__(256) void cached_join_splits_kernel(CachedAttention
 __global__ __launch_bounds__(256) void cached_weights_kernel(CachedAttention a, Plan p, int chunks) {
     const int h = blockIdx.x / chunks % a.c.n_kv, b = blockIdx.x / chunks / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
-    const int rows = st.n * p.group, slot = (blockIdx.x % chunks * 256 + threadIdx.x) * 4;
+    const int rows = st.n * p.group.n, slot = (blockIdx.x % chunks * 256 + threadIdx.x) * 4;
     const size_t unit = ((size_t)b * a.c.n_kv + h) * p.rows_pad;
     if (slot >= st.len) return;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
@@ -898,8 +906,8 @@ struct SharedLoads {
 };
 
 // the slots that rows r0 .. r1 of a state can see at all end here
-__device__ __forceinline__ int end_of_sight(const CachedAttention& a, const StateTokens& st, int group, int r1) {
-    const int n = a.tree ? st.len : st.base + r1 / group + 1;
+__device__ __forceinline__ int end_of_sight(const CachedAttention& a, const StateTokens& st, const Group& group, int r1) {
+    const int n = a.tree ? st.len : st.base + group.token(r1) + 1;
     return n < 0 ? 0 : n;
 }
 
@@ -914,7 +922,7 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
     const int units = a.t.B * a.c.n_kv, unit = blockIdx.x % units, split = blockIdx.x / units % p.splits;
     const int rb = p.row_blocks - 1 - (int)(blockIdx.x / units) / p.splits, h = unit % a.c.n_kv, b = unit / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
-    const int rows = st.n * p.group, r0 = rb * ROWS;
+    const int rows = st.n * p.group.n, r0 = rb * ROWS;
     if (r0 >= rows) return;
     const int r1 = (r0 + ROWS < rows ? r0 + ROWS : rows) - 1;
     const int blocks = (end_of_sight(a, st, p.group, r1) + 31) >> 5, per = (blocks + p.splits - 1) / p.splits;
@@ -949,7 +957,7 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
     const int w0 = r0 + wave * 16 * RT, w1 = w0 + 16 * RT - 1 < r1 ? w0 + 16 * RT - 1 : r1;
     const bool busy = w0 <= r1;
     const int wave_blocks = busy ? (end_of_sight(a, st, p.group, w1) + 31) >> 5 : 0;
-    const int all_see = st.base + (a.tree ? 0 : w0 / p.group + 1);
+    const int all_see = st.base + (a.tree ? 0 : p.group.token(w0) + 1);
     RowState<S> row[RT];
     v8h qh[RT][S::KS], ql[RT][S::KS];
     int token[RT];
@@ -957,8 +965,8 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
     for (int r = 0; r < RT; ++r) {
         row[r].clear();
         const int rr = w0 + r * 16 + c;
-        token[r] = (rr < rows ? rr : rows - 1) / p.group;
-        const QueryRow from(a, st, h, p.group, rr < rows ? rr : rows - 1);
+        token[r] = p.group.token(rr < rows ? rr : rows - 1);
+        const QueryRow from(a, st, h, p.group, rr < rows ? rr : rows - 1, token[r], rope_position(a.t, st.row0 + token[r], st.base + token[r]));
 #pragma unroll
         for (int s = 0; s < S::KS; ++s) {
             QueryPart<S> q;
@@ -1112,7 +1120,7 @@ __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAtten
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int unit = blockIdx.x / chunks, h = unit % a.c.n_kv, b = unit / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
-    const int rows = st.n * p.group, slot0 = (blockIdx.x % chunks * 4 + wave) * 32;
+    const int rows = st.n * p.group.n, slot0 = (blockIdx.x % chunks * 4 + wave) * 32;
     if (rows == 0 || slot0 >= st.len) return;
     const int lo = kv_row_index(a.c, b, h, slot0), hi = slot0 + 16 < st.len ? kv_row_index(a.c, b, h, slot0 + 16) : -1;
     const int n = st.len - slot0;
@@ -1135,7 +1143,7 @@ __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAtten
     const uint32_t mine = bits_of_group(there, g);
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const int token0 = a.tree || slot0 <= st.base ? 0 : slot0 - st.base;          // the first token that sees the block's first slot
-    for (int rt = token0 * p.group / 16; rt * 16 < rows; ++rt) {
+    for (int rt = token0 * p.group.n / 16; rt * 16 < rows; ++rt) {
         const uint4* q = p.q + (((size_t)unit * p.rows_pad / 16 + rt) * S::KS * 2) * 64 + lane;
         const int r = rt * 16 + c;
         const float lse = r < rows ? p.lse[(size_t)unit * p.rows_pad + r] : INFINITY;
@@ -1150,9 +1158,9 @@ __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAtten
                 acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[t][s][0], qh, acc[t], 0, 0, 0);
             }
         }
-        const int token = (r < rows ? r : rows - 1) / p.group;
+        const int token = p.group.token(r < rows ? r : rows - 1);
         uint32_t bits = mine;
-        if (slot0 + 32 > st.base + (a.tree ? 0 : rt * 16 / p.group + 1)) bits &= bits_of_group(visible_bits(a, st, token, slot0), g);
+        if (slot0 + 32 > st.base + (a.tree ? 0 : p.group.token(rt * 16) + 1)) bits &= bits_of_group(visible_bits(a, st, token, slot0), g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             float x = acc[e >> 2][e & 3];
@@ -1183,8 +1191,9 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
     Layout L;
     memset(&L, 0, sizeof(L));
     Plan& p = L.p;
-    p.group = n_heads / c.n_kv;
-    p.rows_max = max_new * p.group;
+    p.group.n = n_heads / c.n_kv;
+    p.group.inverse = p.group.n == 1 ? 0u : (uint32_t)(((1ull << 32) + p.group.n - 1) / p.group.n);
+    p.rows_max = max_new * p.group.n;
     p.splits = 1;
     const int units = B * c.n_kv, blocks = (max_len + 31) / 32;
     // 16 rows fill one column block of the matrix instructions; more would have a wavefront of the first form hold two.  20 rows, 64
