@@ -262,49 +262,66 @@ struct QueryRow {
         sn = a.t.sin_t + (size_t)pos * (dh / 2);
     }
 };
-// Eight components d0 .. of a query row, rotated, scaled and split into an operand's hi and lo words.  Fragments hold, in lane
-// 16 g + c, components 32 s + 8 g .. of row c.
+// Four components d0 .. of a query row, rotated, scaled and split into an operand's hi and lo words.
 template <class S>
-struct QueryPart {
-    float x[8], y[8], c[8], w[8];      // components, their partners, cosines, sines
-    __device__ __forceinline__ void request(const float* q, const float* ct, const float* sn, int d0) {
+struct QueryFour {
+    float x[4], y[4], c[4], w[4];      // components, their partners, cosines, sines
+    __device__ __forceinline__ void request(const QueryRow& q, int d0) {
         constexpr int DH = S::DH, half = DH / 2;
-        if constexpr (DH % 16 == 0) {                                  // eight components lie in one half
+        if constexpr (DH % 8 == 0) {                                   // four components lie in one half
             const int d = d0 < DH ? d0 : 0, f = d < half ? d : d - half, partner = d < half ? d + half : d - half;
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                *reinterpret_cast<float4*>(x + e) = *reinterpret_cast<const float4*>(q + d + e);
-                *reinterpret_cast<float4*>(y + e) = *reinterpret_cast<const float4*>(q + partner + e);
-                *reinterpret_cast<float4*>(c + e) = *reinterpret_cast<const float4*>(ct + f + e);
-                *reinterpret_cast<float4*>(w + e) = *reinterpret_cast<const float4*>(sn + f + e);
-            }
+            *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(q.x + d);
+            *reinterpret_cast<float4*>(y) = *reinterpret_cast<const float4*>(q.x + partner);
+            *reinterpret_cast<float4*>(c) = *reinterpret_cast<const float4*>(q.ct + f);
+            *reinterpret_cast<float4*>(w) = *reinterpret_cast<const float4*>(q.sn + f);
         } else {                                                       // two do
             static_assert(DH % 4 == 0, "pairs do not straddle the halves");
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
+            for (int e = 0; e < 4; e += 2) {
                 const int d = d0 + e < DH ? d0 + e : 0, f = d < half ? d : d - half, partner = d < half ? d + half : d - half;
-                *reinterpret_cast<float2*>(x + e) = *reinterpret_cast<const float2*>(q + d);
-                *reinterpret_cast<float2*>(y + e) = *reinterpret_cast<const float2*>(q + partner);
-                *reinterpret_cast<float2*>(c + e) = *reinterpret_cast<const float2*>(ct + f);
-                *reinterpret_cast<float2*>(w + e) = *reinterpret_cast<const float2*>(sn + f);
+                *reinterpret_cast<float2*>(x + e) = *reinterpret_cast<const float2*>(q.x + d);
+                *reinterpret_cast<float2*>(y + e) = *reinterpret_cast<const float2*>(q.x + partner);
+                *reinterpret_cast<float2*>(c + e) = *reinterpret_cast<const float2*>(q.ct + f);
+                *reinterpret_cast<float2*>(w + e) = *reinterpret_cast<const float2*>(q.sn + f);
             }
         }
     }
-    __device__ __forceinline__ void split(bool live, int d0, uint4& hi, uint4& lo) const {
+    __device__ __forceinline__ void split(bool live, int d0, uint2& hi, uint2& lo) const {
         constexpr int DH = S::DH, half = DH / 2;
         const float scale = (float)(1.0 / sqrt((double)DH)) * LOG2E;
-        float z[8];
+        float z[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4; ++e) {
             const float p = y[e] * w[e];
             z[e] = live && d0 + e < DH ? (x[e] * c[e] + (d0 + e < half ? -p : p)) * scale : 0.f;
         }
         split_pair(z[0], z[1], hi.x, lo.x);
         split_pair(z[2], z[3], hi.y, lo.y);
-        split_pair(z[4], z[5], hi.z, lo.z);
-        split_pair(z[6], z[7], hi.w, lo.w);
     }
 };
+// Components 32 s + 8 g .. + 7 of the rows of a query tile, for lane 16 g + c of row c.  ONE_BY_ONE: four and four, in half the registers.
+template <class S, bool ONE_BY_ONE>
+struct QueryPart {
+    QueryFour<S> q[ONE_BY_ONE ? 1 : 2];
+    __device__ __forceinline__ void request(const QueryRow& from, int d0) {
+        q[0].request(from, d0);
+        if constexpr (!ONE_BY_ONE) q[1].request(from, d0 + 4);
+    }
+    __device__ __forceinline__ void split(const QueryRow& from, bool live, int d0, uint4& hi, uint4& lo) {
+        uint2 a, b, c, d;
+        q[0].split(live, d0, a, b);
+        if constexpr (ONE_BY_ONE) {
+            __builtin_amdgcn_sched_barrier(0);
+            q[0].request(from, d0 + 4);
+            q[0].split(live, d0 + 4, c, d);
+        } else {
+            q[1].split(live, d0 + 4, c, d);
+        }
+        hi = make_uint4(a.x, a.y, c.x, c.y);
+        lo = make_uint4(b.x, b.y, d.x, d.y);
+    }
+};
+
 // which of the slots slot0 .. slot0 + 31 token i sees, for blocks that not every row sees whole
 __device__ __forceinline__ uint32_t visible_bits(const CachedAttention& a, const StateTokens& st, int i, int slot0) {
     if (!a.tree) {
@@ -568,11 +585,9 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
     for (;;) {
         const int rows = st.n * p.group.n, seen = st.len;                // (the last token sees them all, or bits of the mask)
         const bool all = first == 0 && last == blocks, live = c < rows;
-        QueryPart<S> q;
-        if (threadIdx.x < JOBS) {
-            const QueryRow from(a, st, h, p.group, query_row(), token, pos);
-            q.request(from.x, from.ct, from.sn, d0);
-        }
+        const QueryRow from(a, st, h, p.group, query_row(), token, pos);
+        QueryPart<S, DT == BRL_F32> q;                                 // (fp32: the blocks under way leave no registers for all of it)
+        if (threadIdx.x < JOBS) q.request(from, d0);
         // where this wavefront's first block of the next segment lies
         left -= last - first;
         if (p.groups == 0) left = 0;
@@ -593,7 +608,7 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         const int all_see = st.base + (a.tree ? 0 : 1);                // slots below are seen by every row (causal: by token 0)
         if (threadIdx.x < JOBS) {
             uint4 x, y;
-            q.split(live, d0, x, y);
+            q.split(from, live, d0, x, y);
             store_query<S>(s_q, wave, lane, x, y);
         }
         after_lo = __builtin_amdgcn_readfirstlane(after_lo);
@@ -969,10 +984,10 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
         const QueryRow from(a, st, h, p.group, rr < rows ? rr : rows - 1, token[r], rope_position(a.t, st.row0 + token[r], st.base + token[r]));
 #pragma unroll
         for (int s = 0; s < S::KS; ++s) {
-            QueryPart<S> q;
-            q.request(from.x, from.ct, from.sn, 32 * s + 8 * g);
+            QueryPart<S, false> q;
+            q.request(from, 32 * s + 8 * g);
             uint4 x, y;
-            q.split(rr < rows, 32 * s + 8 * g, x, y);
+            q.split(from, rr < rows, 32 * s + 8 * g, x, y);
             qh[r][s] = __builtin_bit_cast(v8h, x);
             ql[r][s] = __builtin_bit_cast(v8h, y);
             if (p.q && split == 0 && w0 + r * 16 <= r1)
