@@ -564,18 +564,17 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         f[1] = *reinterpret_cast<const float4*>(pool + (x_hi < 0 ? 0 : x_hi) + (unsigned)(4 * g));
     };
     int page_lo = -1, page_hi = -1;                                    // rows of the lane-th block ahead
-    auto pages = [&](int t0) {
-        const int block = t0 + lane * waves, slot = block * 32;
+    auto pages = [&](int t0, int from) {                               // from: this lane
+        const int block = t0 + from * waves, slot = block * 32;
         page_lo = block < last && slot < st.len ? kv_row_index(a.c, b, h, slot) : -1;
         page_hi = block < last && slot + 16 < st.len ? kv_row_index(a.c, b, h, slot + 16) : -1;
     };
     constexpr int JOBS = S::KS * 64;                                   // query fragments: a lane of a step each, of the first threads
     static_assert(JOBS <= 256, "every workgroup has the threads");
-    const int d0 = 32 * wave + 8 * g;
-    auto query_row = [&]() { return c < st.n * p.group.n ? c : st.n * p.group.n - 1; };
+    auto query_row = [&](int c) { return c < st.n * p.group.n ? c : st.n * p.group.n - 1; };
     auto position = [&](int token) { return rope_position(a.t, st.row0 + token, st.base + token); };
-    int token = p.group.token(query_row()), pos = position(token);
-    pages(first + wave);
+    int token = p.group.token(query_row(c)), pos = position(token);
+    pages(first + wave, lane);
     int lo = lane_value(page_lo, 0), hi = lane_value(page_hi, 0);      // where the block under way lies
     keys.request(a.c.k, lo, hi, lane);
     if constexpr (DT == BRL_I8) scales(a.c.ks, lo, hi, ks);
@@ -583,9 +582,12 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
     if constexpr (DT == BRL_I8) scales(a.c.vs, lo, hi, vs);
     bool before = true;                                                // nothing but this segment's beginning lies in front
     for (;;) {
+        int here = lane;                                               // (opaque: nothing that a segment needs is kept from one to the next)
+        asm volatile("" : "+v"(here));
+        const int c = here & 15, g = here >> 4, d0 = 32 * wave + 8 * g;
         const int rows = st.n * p.group.n, seen = st.len;                // (the last token sees them all, or bits of the mask)
         const bool all = first == 0 && last == blocks, live = c < rows;
-        const QueryRow from(a, st, h, p.group, query_row(), token, pos);
+        const QueryRow from(a, st, h, p.group, query_row(c), token, pos);
         QueryPart<S, DT == BRL_F32> q;                                 // (fp32: the blocks under way leave no registers for all of it)
         if (threadIdx.x < JOBS) q.request(from, d0);
         // where this wavefront's first block of the next segment lies
@@ -609,7 +611,7 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         if (threadIdx.x < JOBS) {
             uint4 x, y;
             q.split(from, live, d0, x, y);
-            store_query<S>(s_q, wave, lane, x, y);
+            store_query<S>(s_q, wave, here, x, y);
         }
         after_lo = __builtin_amdgcn_readfirstlane(after_lo);
         after_hi = __builtin_amdgcn_readfirstlane(after_hi);
@@ -633,7 +635,7 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
             // have every wait in the loop wait for all of them.
             if (++ahead == 64) {
                 ahead = 0;
-                pages(t + waves);
+                pages(t + waves, at);
             }
             const bool more = t + waves < last;
             const int next_lo = more ? lane_value(page_lo, ahead) : after_lo, next_hi = more ? lane_value(page_hi, ahead) : after_hi;
@@ -737,8 +739,8 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         blocks = blocks_of(st);
         first = 0;
         last = left < blocks ? left : blocks;
-        pages(wave);
-        token = p.group.token(query_row());
+        pages(wave, here);
+        token = p.group.token(query_row(c));
         pos = position(token);
     }
 }
