@@ -189,7 +189,8 @@ __device__ __forceinline__ Before scan_before(uint32_t a, uint32_t b, uint2* wav
 
 // HELD: quads of weights that a thread keeps in registers (4 HELD neighbouring slots, all of a list in 4096 HELD slots); 0: the list
 // is read again for each pass, 4096 slots at a time.  8000 slots, 320 lists: 20.4 us when every list was read four times.
-template <int HELD>
+// WHOLE: rows of weights start on 16 bytes.
+template <int HELD, bool WHOLE>
 __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a) {
     // Weights crowd into few bins of the first pass (their exponents): eight copies of each bin, side by side in neighbouring
     // banks, so that a wavefront's lanes do not queue for one address.
@@ -209,21 +210,23 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
     const int lo = a.first, hi = len - a.recent;
     const float* w = a.weights + (size_t)blockIdx.x * a.ld;
     uint32_t key[4 * Q];                              // 0 (below every key of a weight) outside lo .. hi - 1
+    // (loads past the list read its row's end, not used: a load that might not happen is waited for before the next)
+    const int row_end = a.ld < (size_t)hi + 3 ? (int)a.ld : hi + 3;
     auto read = [&](int i0) {
-        float x[4 * Q];
-        const bool whole = ((a.ld | (size_t)(reinterpret_cast<uintptr_t>(a.weights) >> 2)) & 3) == 0;
+        if constexpr (WHOLE) {
 #pragma unroll
-        for (int j = 0; j < Q; ++j) {
-            const int i = i0 + 4 * j;
-            if (whole && i + 4 <= hi) {
-                *reinterpret_cast<float4*>(x + 4 * j) = *reinterpret_cast<const float4*>(w + i);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[4 * j + e] = i + e < hi ? w[i + e] : 0.f;
+            for (int j = 0; j < Q; ++j) {
+                const int i = i0 + 4 * j, at = i + 4 <= row_end ? i : (row_end & ~3) - 4;
+                const float4 x = *reinterpret_cast<const float4*>(w + (at < 0 ? 0 : at));
+                key[4 * j] = __float_as_uint(x.x); key[4 * j + 1] = __float_as_uint(x.y);
+                key[4 * j + 2] = __float_as_uint(x.z); key[4 * j + 3] = __float_as_uint(x.w);
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4 * Q; ++e) key[e] = __float_as_uint(w[i0 + e < hi ? i0 + e : hi - 1]);
         }
 #pragma unroll
-        for (int e = 0; e < 4 * Q; ++e) key[e] = i0 + e >= lo && i0 + e < hi ? weight_key(x[e]) : 0u;
+        for (int e = 0; e < 4 * Q; ++e) key[e] = weight_key(__uint_as_float(key[e])) & ((unsigned)(i0 + e - lo) < (unsigned)(hi - lo) ? ~0u : 0u);
     };
     const int steps = HELD ? 1 : (hi + 4 * SEL_THREADS - 1) / (4 * SEL_THREADS);
     if (HELD) read(tid * 4 * Q);
@@ -240,8 +243,10 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
         for (int step = 0; step < steps; ++step) {
             if (!HELD) read((step * SEL_THREADS + tid) * 4);
 #pragma unroll
-            for (int e = 0; e < 4 * Q; ++e)
+            for (int e = 0; e < 4 * Q; ++e) {
+                if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
                 if (key[e] && (pass == 0 || key[e] >> above == prefix)) atomicAdd(&hist[((key[e] >> shift) & ((1u << bits) - 1)) * SEL_COPIES + tid % SEL_COPIES], 1u);
+            }
         }
         __syncthreads();
         // bins from the top: thread t has bins top - 2 t and top - 2 t - 1
@@ -274,6 +279,7 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
         uint32_t gb = greater + s.a, qb = equal + s.b;
 #pragma unroll
         for (int e = 0; e < 4 * Q; ++e) {
+            if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
             const bool over = key[e] > prefix, same = key[e] == prefix;
             if (over || (same && qb < want)) kept[a.first + gb + (qb < want ? qb : want)] = i0 + e;
             gb += over;
@@ -379,18 +385,25 @@ int launch_cache_append(const KvView& c, const NewTokens& t, const float* qkv, i
     return c.dtype == BRL_F32 ? append_typed<BRL_F32>(a, s) : c.dtype == BRL_F16 ? append_typed<BRL_F16>(a, s) : append_typed<BRL_I8>(a, s);
 }
 
+template <bool WHOLE>
+static void select_held(const SelectArgs& a, int lists, hipStream_t s) {
+    const dim3 grid((unsigned)lists), block(SEL_THREADS);
+    constexpr int ONE = 4 * SEL_THREADS;
+    if (a.max_len <= ONE) hipLaunchKernelGGL((cache_select_kernel<1, WHOLE>), grid, block, 0, s, a);
+    else if (a.max_len <= 2 * ONE) hipLaunchKernelGGL((cache_select_kernel<2, WHOLE>), grid, block, 0, s, a);
+    else if (a.max_len <= 4 * ONE) hipLaunchKernelGGL((cache_select_kernel<4, WHOLE>), grid, block, 0, s, a);
+    else if (a.max_len <= 16 * ONE) hipLaunchKernelGGL((cache_select_kernel<16, WHOLE>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((cache_select_kernel<0, WHOLE>), grid, block, 0, s, a);
+}
+
 int launch_cache_select(const float* weights, size_t ld_weights, int B, int n_kv, const int32_t* lens, int max_len, int keep,
                         int first, int recent, int32_t* kept, int32_t* counts, hipStream_t s) {
     SelectArgs a;
     a.weights = weights; a.ld = ld_weights; a.lens = lens; a.n_kv = n_kv; a.max_len = max_len; a.keep = keep;
     a.first = first; a.recent = recent; a.kept = kept; a.counts = counts;
     LaunchTimer tm(BRL_KC_ATTENTION, s);
-    const dim3 grid((unsigned)(B * n_kv)), block(SEL_THREADS);
-    if (max_len <= 1 * 4 * SEL_THREADS) hipLaunchKernelGGL(cache_select_kernel<1>, grid, block, 0, s, a);
-    else if (max_len <= 2 * 4 * SEL_THREADS) hipLaunchKernelGGL(cache_select_kernel<2>, grid, block, 0, s, a);
-    else if (max_len <= 4 * 4 * SEL_THREADS) hipLaunchKernelGGL(cache_select_kernel<4>, grid, block, 0, s, a);
-    else if (max_len <= 16 * 4 * SEL_THREADS) hipLaunchKernelGGL(cache_select_kernel<16>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(cache_select_kernel<0>, grid, block, 0, s, a);
+    const bool whole = ((ld_weights | (size_t)(reinterpret_cast<uintptr_t>(weights) >> 2)) & 3) == 0;
+    whole ? select_held<true>(a, B * n_kv, s) : select_held<false>(a, B * n_kv, s);
     BRL_LAUNCH_CHECK("cache_select_kernel");
     return BRL_OK;
 }
