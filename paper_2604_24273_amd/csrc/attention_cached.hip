@@ -436,7 +436,7 @@ struct Plan {
     float* part_o;            // [2 groups][rows_pad][dh]: sums relative to part_ml's reference
     float2* part_ml;          // [2 groups][rows_pad]: reference and sum of probabilities
     float* lse;               // [B][n_kv][rows_pad] or nullptr: log2 of a row's sum, +inf where it sees nothing
-    float* scores;            // [B][n_kv][rows_pad][ld_scores] or nullptr
+    float* scores;            // few rows with weights: [B][n_kv][rows_max][ld_scores], else nullptr
     size_t ld_scores;
 };
 
@@ -673,7 +673,7 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
             hi = next_hi;
             if (!mine) break;
             if (p.scores && live) {
-                float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_pad + c) * p.ld_scores + slot0 + 4 * g;
+                float* f = p.scores + (((size_t)b * a.c.n_kv + h) * p.rows_max + c) * p.ld_scores + slot0 + 4 * g;
                 reinterpret_cast<float4*>(f)[0] = make_float4(s[0], s[1], s[2], s[3]);
                 reinterpret_cast<float4*>(f)[4] = make_float4(s[4], s[5], s[6], s[7]);
             }
@@ -836,13 +836,13 @@ __global__ __launch_bounds__(256) void cached_weights_kernel(CachedAttention a, 
     const int h = blockIdx.x / chunks % a.c.n_kv, b = blockIdx.x / chunks / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
     const int rows = st.n * p.group.n, slot = (blockIdx.x % chunks * 256 + threadIdx.x) * 4;
-    const size_t unit = ((size_t)b * a.c.n_kv + h) * p.rows_pad;
+    const size_t unit = (size_t)b * a.c.n_kv + h;
     if (slot >= st.len) return;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int r = 0; r < rows; ++r) {
-        const float4 s = *reinterpret_cast<const float4*>(p.scores + (unit + r) * p.ld_scores + slot);
-        const float lse = p.lse[unit + r];
+        const float4 s = *reinterpret_cast<const float4*>(p.scores + (unit * p.rows_max + r) * p.ld_scores + slot);
+        const float lse = p.lse[unit * p.rows_pad + r];
         w[0] += __builtin_amdgcn_exp2f(s.x - lse);
         w[1] += __builtin_amdgcn_exp2f(s.y - lse);
         w[2] += __builtin_amdgcn_exp2f(s.z - lse);
@@ -1262,7 +1262,7 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
             L.q_off = take(rows * ((c.dh + 31) / 32) * 32 * 4);
         } else {
             p.ld_scores = (size_t)blocks * 32;
-            L.scores_off = take(rows * p.ld_scores * 4);
+            L.scores_off = take((size_t)units * p.rows_max * p.ld_scores * 4);
         }
     }
     L.total = off;
