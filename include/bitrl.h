@@ -396,7 +396,8 @@ int attention_forward(const float* qkv, int B, int S,
  *   prefix, evaluated together); tokens from 32 * mask_words on are not seen.
  *   A token that sees nothing gives zeros.  The cache's values within
  *   |x| < 65504 (BRL_F32: fp16 hi + lo pairs on the matrix cores, as in
- *   BRL_ATTN_MFMA).
+ *   BRL_ATTN_MFMA).  What is infinite or NaN in a slot reaches the tokens that see
+ *   the slot and no others.
  *   weights, DEVICE [B, n_kv_heads, ld_weights] or NULL: weights[b, h, j] += sum
  *   over the state's new tokens and the query heads of k/v head h of the softmax
  *   weight of slot j, in a fixed order.

@@ -518,6 +518,65 @@ def test_an_fp32_cache_gives_what_whole_states_give(dh, hq, hkv, theta):
         assert np.abs(got - part).max() <= 2 * REL * np.abs(part).max()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "i8"])
+@pytest.mark.parametrize("mask", ["causal", "tree"])
+@pytest.mark.parametrize("dh,hq,hkv,page,cached,new", [
+    (128, 4, 4, 16, [40, 0, 3], [9, 5, 16]),
+    (128, 20, 5, 32, [1700, 31], [3, 2]),                         # the shared list
+    (100, 2, 1, 64, [700, 90, 0], [7, 8, 1]),
+    (16, 8, 2, 16, [20], [4]),
+    (64, 4, 2, 32, [100, 0], [40, 20]),                           # keys shared by many rows
+    (100, 3, 3, 32, [900], [70]),                                 # and split
+    (128, 8, 2, 64, [10, 0], [130, 33]),                          # two row tiles per wavefront
+    (32, 12, 4, 128, [0], [200]),
+])
+def test_infinities_and_nan_stay_with_the_tokens_that_see_them(dh, hq, hkv, page, cached, new, mask, dtype):
+    """New tokens whose values (int8: the scale of a value row) or keys are infinite or NaN: a token that does not see their slots
+    gets what it gets without them; one that does has the components not finite that the sum says.  (What a token gets that sees an
+    infinite key is open: an operand's two halves times infinity can be infinities of either sign.  Keys: the tokens that see none.)"""
+    B, R = _mods()
+    print("strange", dh, hq, hkv, page, cached, new, mask, dtype, flush=True)
+    lens = [a + n for a, n in zip(cached, new)]
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(cu[-1])
+    rng = np.random.default_rng(dh + T)
+    qkv = synth.normal(31, dh + T, (T, (hq + 2 * hkv) * dh))
+    cos, sin = tables(max(lens), dh)
+    words = -(-max(new) // 32)
+    tree = None if mask == "causal" else np.concatenate([ancestors(rng, n, words) for n in new])
+    for name in ("v", "k"):
+        c = make_cache(32, hkv, dh, page, lens, DTYPES[dtype])
+        for b, n in enumerate(new):
+            for i, bad in ((n // 2, np.inf), (n - 1, np.nan), (2 * n // 3, -np.inf)):
+                slot = cached[b] + i
+                pg, at, h = c["table"][b, slot // page], slot % page, i % hkv
+                if dtype == "i8":
+                    c[name + "_scale"][pg, h, at] = bad
+                else:
+                    c[name][pg, h, at, rng.integers(0, dh, 3)] = bad
+        ref = dict(c)
+        if name == "k":                                                   # NaN, which every token that sees it has in all components
+            n = "k_scale" if dtype == "i8" else "k"
+            ref[n] = np.where(np.isinf(c[n]), c[n].dtype.type(np.nan), c[n])
+        with np.errstate(all="ignore"):
+            want, added, reach = K.attend(ref, qkv, hq, cu, lens, None, cos, sin, tree)
+        w = torch.zeros(len(lens), hkv, max(lens), device="cuda")
+        got = OnGpu(B, R, c, dh, cos, sin).attend(qkv, hq, cu, max(new), lens, tree=tree, weights=w)
+        plain = OnGpu(B, R, c, dh, cos, sin).attend(qkv, hq, cu, max(new), lens, tree=tree)
+        finite = np.isfinite(want)
+        assert finite.any() and not finite.all()
+        # reach of rows with something infinite is no bound for their finite components: the largest value there is
+        most = 127 * 1.2 / 42 if dtype == "i8" else max(np.abs(c["v"][np.isfinite(c["v"])].astype(np.float64)).max(), 1.0)
+        bound = REL * np.where(np.isfinite(reach), reach, most)[:, None]
+        for y in (got, plain):
+            assert np.all(np.isfinite(y)[finite]) and (name == "k" or np.array_equal(np.isfinite(y), finite)), name
+            diff = np.abs(y[finite].astype(np.float64) - want[finite])
+            assert np.all(diff <= np.broadcast_to(np.maximum(bound, REL * most), want.shape)[finite]), name
+        if name == "v":
+            g = w.cpu().numpy()[:, :, :added.shape[2]]
+            assert np.all(np.abs(g - added) <= 4e-6 * added + 2.0 ** -23 * g)
+
+
 # ---------------------------------------------------------------- selection and moving
 
 @pytest.mark.parametrize("lens,keep,first,recent", [
@@ -708,3 +767,44 @@ def test_an_episode_prompt_steps_branches_eviction(dtype):
     attend([1, 30])
     attend([1, 1])
     assert np.abs(gw.cpu().numpy() - rw).max() <= 1e-5 * rw.max()
+
+
+# ---------------------------------------------------------------- groups of every size, the same row several times
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "i8"])
+@pytest.mark.parametrize("dh,group,hkv,cached,new", [
+    (32, 3, 2, [70, 5], [5, 4]), (64, 5, 1, [40], [3]), (64, 7, 2, [1100], [2]), (32, 16, 1, [90, 3], [1, 1]), (16, 17, 1, [64, 2], [1, 1]),
+    (32, 48, 1, [33], [3]), (16, 6, 3, [3, 1500], [11, 2]),
+])
+def test_groups_of_every_size(dh, group, hkv, cached, new, dtype):
+    B, R = _mods()
+    print("group", dh, group, hkv, cached, new, dtype, flush=True)
+    hq = group * hkv
+    lens = [a + n for a, n in zip(cached, new)]
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(cu[-1])
+    qkv = synth.normal(51, dh + group, (T, (hq + 2 * hkv) * dh))
+    cos, sin = tables(max(lens), dh)
+    c = make_cache(52, hkv, dh, 16, lens, DTYPES[dtype])
+    w = torch.zeros(len(lens), hkv, max(lens), device="cuda")
+    got = OnGpu(B, R, c, dh, cos, sin).attend(qkv, hq, cu, max(new), lens, weights=w)
+    want, added, reach = K.attend(c, qkv, hq, cu, lens, None, cos, sin)
+    check_rows(got, want, reach, cu, T, len(lens))
+    g = w.cpu().numpy()
+    assert np.all(np.abs(g - added) <= 4e-6 * added + 2.0 ** -23 * g)
+
+
+@pytest.mark.parametrize("ld,shift", [(3001, 0), (3004, 1), (3004, 2), (3000, 0)])
+def test_select_from_rows_on_any_four_bytes(ld, shift):
+    """Rows of weights that do not start on 16 bytes, and the last row of memory that ends with the last slot."""
+    B, R = _mods()
+    w = np.abs(synth.normal(61, ld, (2, 3, ld)))
+    flat = torch.zeros(w.size + 8, device="cuda")
+    flat[shift:shift + w.size] = R.dev(w.ravel())
+    t = flat[shift:shift + w.size].view(2, 3, ld)
+    kept = torch.zeros(2, 3, 500, dtype=torch.int32, device="cuda")
+    counts = torch.zeros(2, dtype=torch.int32, device="cuda")
+    lens = np.array([3000, 2998], np.int32)
+    B.attention_cache_select(t, 2, 3, R.dev(lens), 3000, 500, 3, 50, kept, counts)
+    want, n = K.select(w, lens, 500, 3, 50)
+    assert np.array_equal(kept.cpu().numpy(), want) and np.array_equal(counts.cpu().numpy(), n)
