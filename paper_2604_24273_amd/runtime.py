@@ -176,6 +176,151 @@ class EncoderHandle:
         return h
 
 
+class KVCache:
+    """A paged key/value cache of one layer for a number of states, the pages given out as the states grow.
+
+    append takes the new tokens of every state (qkv rows back to back, `new` how many each state has), attend follows it with
+    their attention over all that the states hold.  With track_weights attend also adds up the attention each slot receives;
+    evict keeps the heaviest slots of states over a budget.  keep_branch keeps some of the last tokens (of a tree of
+    candidates) and drops the rest.  Positions count a state's tokens from its first, whatever has been evicted since.
+    Lengths and pages are kept on the host and sent to the device with every call that changes them, so these calls are not
+    for capture into a graph; the calls of the C ABI that they wrap are."""
+
+    def __init__(self, states: int, n_heads: int, n_kv_heads: int, head_dim: int, max_tokens: int, rope_theta: float,
+                 dtype: torch.dtype = torch.float32, page_tokens: int = 64, n_pages: Optional[int] = None,
+                 max_position: Optional[int] = None, track_weights: bool = False):
+        """max_tokens: slots that a state can have in use at a time.  n_pages: pages of the pool (default: enough for all states
+        at max_tokens).  max_position: positions in the rotary tables (default max_tokens; more where states are evicted)."""
+        if dtype not in (torch.float32, torch.float16, torch.int8):
+            raise ValueError("a cache is float32, float16 or int8")
+        if min(states, n_heads, n_kv_heads, head_dim, max_tokens, page_tokens) < 1:
+            raise ValueError("states, heads, head_dim, max_tokens and page_tokens must be positive")
+        self.states, self.n_heads, self.n_kv_heads, self.head_dim = states, n_heads, n_kv_heads, head_dim
+        self.max_tokens, self.page_tokens, self.table_pages = max_tokens, page_tokens, -(-max_tokens // page_tokens)
+        n_pages = states * self.table_pages if n_pages is None else n_pages
+        shape = (n_pages, n_kv_heads, page_tokens, (head_dim + 15) // 16 * 16)
+        self.k, self.v = (torch.empty(shape, dtype=dtype, device=DEV) for _ in range(2))
+        self.k_scale, self.v_scale = (torch.empty(shape[:3], device=DEV) if dtype == torch.int8 else None for _ in range(2))
+        self.table = torch.full((states, self.table_pages), -1, dtype=torch.int32, device=DEV)
+        self.lens = torch.zeros(states, dtype=torch.int32, device=DEV)
+        self.struct = B.make_kv_cache(self.k, self.v, self.k_scale, self.v_scale, self.table, head_dim)
+        n = max_tokens if max_position is None else max_position
+        self.rope_cos, self.rope_sin = (torch.empty((n, head_dim // 2), device=DEV) for _ in range(2))
+        B.attention_rope_table(self.rope_cos, self.rope_sin, head_dim, rope_theta)
+        self.lens_host = np.zeros(states, dtype=np.int32)       # slots in use
+        self.seen = np.zeros(states, dtype=np.int32)            # tokens that a state has had: its next position
+        self.pages: List[List[int]] = [[] for _ in range(states)]
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.weights = torch.zeros((states, n_kv_heads, max_tokens), device=DEV) if track_weights else None
+        self.ws: Optional[Workspace] = None
+        self._last = None                                       # the last append: rows, tokens, positions, where they began
+
+    def _resize(self, lens: np.ndarray) -> None:
+        """States have `lens` slots from here on: pages are given out or freed; lengths and pages go to the device."""
+        need = [-(-int(n) // self.page_tokens) for n in lens]
+        if sum(need) - sum(len(p) for p in self.pages) > len(self.free):
+            raise MemoryError("the cache has no page left")
+        for p, n in zip(self.pages, need):
+            while len(p) > n:
+                self.free.append(p.pop())
+        for p, n in zip(self.pages, need):
+            while len(p) < n:
+                p.append(self.free.pop())
+        table = np.full((self.states, self.table_pages), -1, dtype=np.int32)
+        for b, p in enumerate(self.pages):
+            table[b, :len(p)] = p
+        self.lens_host = lens.astype(np.int32)
+        self.table.copy_(torch.from_numpy(table))
+        self.lens.copy_(torch.from_numpy(self.lens_host))
+
+    def append(self, qkv: torch.Tensor, new: Sequence[int], depths: Optional[Sequence[int]] = None) -> None:
+        """Stores the keys and values of new[b] tokens per state.  depths: per token its distance behind the state's tokens (of a
+        tree of candidates), None for one after the other."""
+        new = np.asarray(new, dtype=np.int32)
+        width = (self.n_heads + 2 * self.n_kv_heads) * self.head_dim
+        if new.shape != (self.states,) or (new < 0).any() or int(new.sum()) < 1:
+            raise ValueError("new: how many tokens each of the %d states has, one at least in all" % self.states)
+        total = int(new.sum())
+        if qkv.dtype != torch.float32 or tuple(qkv.shape) != (total, width):
+            raise ValueError("qkv must be float32 [%d, %d]" % (total, width))
+        if (self.lens_host.astype(np.int64) + new > self.max_tokens).any():
+            raise ValueError("a state would have more than max_tokens = %d slots in use" % self.max_tokens)
+        cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        steps = np.concatenate([np.arange(n) for n in new]) if depths is None else np.asarray(depths, dtype=np.int64)
+        if steps.shape != (total,) or steps.min() < 0:
+            raise ValueError("depths: one per token, 0 for the first behind the state's tokens")
+        pos = np.repeat(self.seen.astype(np.int64), new) + steps
+        if pos.max() >= self.rope_cos.shape[0]:
+            raise ValueError("a token's position is behind the rotary tables' %d" % self.rope_cos.shape[0])
+        qkv = qkv.contiguous()
+        began = (self.lens_host.copy(), self.seen.copy())
+        self._resize(self.lens_host + new)
+        self._last = (qkv, new, total, dev(cu), dev(pos.astype(np.int32)), began)
+        B.attention_cache_append(self.struct, qkv, self.n_heads, total, self.states, self._last[3], int(new.max()), self.lens,
+                                 self._last[4], self.rope_cos, self.rope_sin)
+        for b in range(self.states):
+            if new[b]:
+                self.seen[b] = int(pos[cu[b]:cu[b + 1]].max()) + 1
+
+    def attend(self, tree_mask: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention [tokens, n_heads * head_dim] of the last append's tokens over everything that their states hold.
+        tree_mask: int32 [tokens, words], bit j of a token's row: it sees its state's new token j."""
+        if self._last is None:
+            raise ValueError("attend follows append")
+        qkv, new, total, cu, pos, _ = self._last
+        if tree_mask is not None and (tree_mask.dtype != torch.int32 or tree_mask.dim() != 2 or tree_mask.shape[0] != total):
+            raise ValueError("tree_mask must be int32 [%d, words]" % total)
+        longest, max_len = int(new.max()), int(self.lens_host.max())
+        need = B.brl_attention_cached_workspace_bytes(self.struct, self.n_heads, total, self.states, longest, max_len,
+                                                      self.weights is not None)
+        self.ws = Workspace(need) if self.ws is None else self.ws.ensure(need)
+        out = torch.empty((total, self.n_heads * self.head_dim), dtype=torch.float32, device=DEV)
+        B.attention_cached_forward(self.struct, qkv, self.n_heads, total, self.states, cu, longest, self.lens, max_len, pos,
+                                   self.rope_cos, self.rope_sin, None if tree_mask is None else tree_mask.contiguous(), out,
+                                   self.weights, self.ws.buf)
+        return out
+
+    def _settle(self, lens: np.ndarray) -> None:
+        """Slots behind `lens` are given up: their pages, and their weights."""
+        self._resize(lens)
+        if self.weights is not None:
+            behind = torch.arange(self.max_tokens, device=DEV) >= self.lens[:, None]
+            self.weights.masked_fill_(behind[:, None, :], 0.0)
+        self._last = None
+
+    def evict(self, keep: int, first: int, recent: int) -> torch.Tensor:
+        """States with more than `keep` slots are cut to it, every k/v head by itself: the first, the last, and between them those
+        with the largest attention so far.  Returns the slots kept, [states, kv heads, keep], -1 behind the last."""
+        if self.weights is None:
+            raise ValueError("evict needs a cache made with track_weights")
+        kept = torch.empty((self.states, self.n_kv_heads, keep), dtype=torch.int32, device=DEV)
+        counts = torch.empty((self.states,), dtype=torch.int32, device=DEV)
+        B.attention_cache_select(self.weights, self.states, self.n_kv_heads, self.lens, self.max_tokens, keep, first, recent,
+                                 kept, counts)
+        B.attention_cache_compact(self.struct, self.states, self.lens, self.max_tokens, kept, self.n_kv_heads, None, counts,
+                                  self.weights)
+        self._settle(np.minimum(self.lens_host, keep))
+        return kept
+
+    def keep_branch(self, branches: Sequence[Sequence[int]]) -> None:
+        """Of the last append's tokens of each state those whose indices (ascending) are given stay, one behind the other, and
+        the state goes on behind them; the rest is dropped."""
+        if self._last is None:
+            raise ValueError("keep_branch follows append")
+        new, (start, seen) = self._last[1], self._last[5]
+        if len(branches) != self.states or any(list(x) != sorted(set(x)) or (len(x) and not 0 <= x[0] <= x[-1] < n)
+                                               for x, n in zip(branches, new)):
+            raise ValueError("a branch is ascending indices of the state's last tokens, one list per state")
+        counts = np.array([len(x) for x in branches], dtype=np.int32)
+        kept = np.full((self.states, 1, max(1, int(counts.max()))), -1, dtype=np.int32)
+        for b, x in enumerate(branches):
+            kept[b, 0, :len(x)] = start[b] + np.asarray(x, dtype=np.int32)
+        B.attention_cache_compact(self.struct, self.states, self.lens, self.max_tokens, dev(kept), 1, dev(start), dev(counts),
+                                  self.weights)
+        self._settle(start + counts)
+        self.seen = seen + counts
+
+
 class HeadHandle:
     def __init__(self, shape: synth.EncoderShape, seed: int = 0, act: int = B.BRL_ACT_TANH):
         pw, pb = synth.head_params(seed, shape, "policy")

@@ -769,6 +769,117 @@ def test_an_episode_prompt_steps_branches_eviction(dtype):
     assert np.abs(gw.cpu().numpy() - rw).max() <= 1e-5 * rw.max()
 
 
+# ---------------------------------------------------------------- the holder
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "i8"])
+def test_the_holder_through_an_episode(dtype):
+    """runtime.KVCache with fewer pages than its states could fill: pages freed by one state are given to another; every output against
+    the oracle on the cache's own arrays, every stored row against the oracle's."""
+    B, R = _mods()
+    hq, hkv, dh, page, theta = 6, 2, 64, 16, 10000.0
+    kv = R.KVCache(3, hq, hkv, dh, 150, theta, dtype={"f32": torch.float32, "f16": torch.float16, "i8": torch.int8}[dtype], page_tokens=page,
+                   n_pages=17, max_position=300, track_weights=True)
+    for x in (kv.k, kv.v, kv.k_scale, kv.v_scale):
+        if x is not None:
+            x.fill_(7 if x.dtype == torch.int8 else float("nan"))
+    cos, sin = kv.rope_cos.cpu().numpy(), kv.rope_sin.cpu().numpy()
+    c64, s64 = tables(300, dh, theta)
+    assert np.abs(cos - c64).max() < 1e-6 and np.abs(sin - s64).max() < 1e-6
+    rw, seen, turn = np.zeros((3, hkv, 150)), np.zeros(3, int), [0]
+
+    def arrays():
+        c = {"k": kv.k, "v": kv.v, "k_scale": kv.k_scale, "v_scale": kv.v_scale, "table": kv.table}
+        return {n: x.cpu().numpy().copy() for n, x in c.items() if x is not None}
+
+    def step(new, depths=None, tree=None):
+        turn[0] += 1
+        cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        qkv = synth.normal(41, turn[0], (int(cu[-1]), (hq + 2 * hkv) * dh))
+        before = arrays()
+        kv.append(R.dev(qkv), new, depths)
+        out = kv.attend(None if tree is None else R.dev(tree.view(np.int32))).cpu().numpy()
+        pos = np.repeat(seen, new) + (np.concatenate([np.arange(n) for n in new]) if depths is None else np.asarray(depths))
+        c = arrays()
+        before["table"] = c["table"]
+        K.append(before, qkv, hq, cu, kv.lens_host, pos, cos, sin)
+        for n in c:
+            assert same_bits(c[n], before[n]), n
+        want, added, reach = K.attend(c, qkv, hq, cu, kv.lens_host, pos, cos, sin, tree)
+        check_rows(out, want, reach, cu, len(qkv), 3)
+        rw[:, :, :added.shape[2]] += added
+        if depths is None:
+            seen[:] += new
+        assert np.array_equal(kv.lens.cpu().numpy(), kv.lens_host)
+
+    step([100, 20, 0])
+    step([1, 1, 1])
+    step([30, 0, 2])                                                      # 131, 21 and 3 slots: 9, 2 and 1 pages
+    with pytest.raises(MemoryError, match="no page left"):
+        kv.append(torch.zeros(120, (hq + 2 * hkv) * dh, device="cuda"), [0, 120, 0])
+    assert list(kv.lens_host) == [131, 21, 3] and list(kv.seen) == [131, 21, 3]
+    lens, weights, was = kv.lens_host.copy(), kv.weights.cpu().numpy(), arrays()
+    assert np.abs(weights - rw).max() <= 1e-5 * rw.max()
+    kept = kv.evict(40, 2, 10).cpu().numpy()
+    want, counts = K.select(weights, lens, 40, 2, 10)
+    assert np.array_equal(kept, want) and list(kv.lens_host) == [40, 21, 3] and len(kv.free) == 17 - 3 - 2 - 1
+    K.compact(was, lens, want, None, counts, rw)
+    rw[0, :, 40:] = 0
+    now = arrays()
+    for n in now:
+        if n != "table":
+            assert same_bits(now[n], was[n]), n
+    assert not kv.weights[0, :, 40:].any()
+    step([1, 120, 3])                                                     # state 1 on the pages that state 0 gave up
+    # three candidates of two tokens behind state 0, two of one behind state 2
+    tree = np.array([1, 3, 4, 12, 16, 48, 1, 2], np.uint32)[:, None]
+    step([6, 0, 2], [0, 1, 0, 1, 0, 1, 0, 0], tree)
+    start = kv.lens_host - [6, 0, 2]
+    before, lens = arrays(), kv.lens_host.copy()
+    kv.keep_branch([[2, 3], [], [1]])
+    branch = np.array([[[start[0] + 2, start[0] + 3]], [[-1, -1]], [[start[2] + 1, -1]]], np.int32)
+    K.compact(before, lens, branch, start, [2, 0, 1], rw)
+    now = arrays()
+    for n in now:
+        if n != "table":
+            assert same_bits(now[n], before[n]), n
+    seen[:] += [2, 0, 1]
+    assert list(kv.seen) == list(seen) and np.array_equal(kv.lens_host, start + [2, 0, 1])
+    for b in range(3):
+        rw[b, :, kv.lens_host[b]:] = 0
+    step([2, 1, 30])
+    assert np.abs(kv.weights.cpu().numpy() - rw).max() <= 1e-5 * rw.max()
+
+
+def test_the_holder_refuses():
+    B, R = _mods()
+    for bad in (dict(dtype=torch.bfloat16), dict(states=0), dict(head_dim=0), dict(max_tokens=0)):
+        with pytest.raises(ValueError):
+            R.KVCache(**{**dict(states=2, n_heads=4, n_kv_heads=2, head_dim=32, max_tokens=40, rope_theta=1e4, page_tokens=16), **bad})
+    kv = R.KVCache(2, 4, 2, 32, 40, 1e4, page_tokens=16)
+    rows = lambda n: torch.zeros(n, 8 * 32, device="cuda")  # noqa: E731
+    for qkv, new, depths, word in ((rows(2), [1], None, "new"), (rows(2), [3, -1], None, "new"), (rows(0), [0, 0], None, "new"),
+                                   (rows(3), [1, 1], None, "qkv"), (rows(2).half(), [1, 1], None, "qkv"), (rows(42), [41, 1], None, "max_tokens"),
+                                   (rows(2), [1, 1], [0], "depths"), (rows(2), [1, 1], [0, -1], "depths"), (rows(2), [1, 1], [0, 40], "rotary")):
+        with pytest.raises(ValueError, match=word):
+            kv.append(qkv, new, depths)
+    with pytest.raises(ValueError, match="append"):
+        kv.attend()
+    with pytest.raises(ValueError, match="append"):
+        kv.keep_branch([[], []])
+    with pytest.raises(ValueError, match="track_weights"):
+        kv.evict(4, 0, 0)
+    kv.append(rows(3), [2, 1])
+    for bad in ([[0]], [[1, 0], []], [[0, 0], []], [[2], []], [[], [-1]]):
+        with pytest.raises(ValueError, match="branch"):
+            kv.keep_branch(bad)
+    with pytest.raises(ValueError, match="tree_mask"):
+        kv.attend(torch.zeros(2, 1, dtype=torch.int32, device="cuda"))
+    kv.attend()
+    kv.keep_branch([[1], [0]])
+    with pytest.raises(ValueError, match="append"):
+        kv.attend()
+
+
 # ---------------------------------------------------------------- groups of every size, the same row several times
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "i8"])
