@@ -139,7 +139,7 @@ int append_typed(AppendArgs a, hipStream_t s) {
 // One workgroup per list.  The threshold (the key of the last slot that is taken) is found bit group by bit group: a histogram
 // of the next bits of the keys that agree with the threshold so far, scanned from the top.  Then one pass in slot order takes
 // what lies above it and the first of those equal to it.
-constexpr int SEL_THREADS = 1024, SEL_BINS = 2048, SEL_COPIES = 8;
+constexpr int SEL_THREADS = 1024, SEL_BINS = 2048, SEL_COPIES = 8, PARTS = SEL_THREADS / 64;
 
 struct SelectArgs {
     const float* weights;
@@ -166,38 +166,28 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
     v += __builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);       // lane 31's to rows 2 and 3
     return v;
 }
-// sums over the workgroup of what lies in front of this thread, for two numbers, and the totals
-struct Before {
-    uint32_t a, b, all_a, all_b;
-};
-__device__ __forceinline__ Before scan_before(uint32_t a, uint32_t b, uint2* waves) {
+// sum over the workgroup of what lies in front of this thread
+__device__ __forceinline__ uint32_t scan_before(uint32_t a, uint32_t* waves) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t x = wave_scan(a), y = wave_scan(b);
-    if (lane == 63) waves[wave] = make_uint2(x, y);
+    const uint32_t x = wave_scan(a);
+    if (lane == 63) waves[wave] = x;
     __syncthreads();
-    // every wavefront scans the wavefronts' totals itself
-    const uint2 t = waves[lane % (SEL_THREADS / 64)];
-    const uint32_t p = wave_scan(lane < SEL_THREADS / 64 ? t.x : 0u), q = wave_scan(lane < SEL_THREADS / 64 ? t.y : 0u);
-    Before r;
-    r.all_a = lane_value(p, SEL_THREADS / 64 - 1);
-    r.all_b = lane_value(q, SEL_THREADS / 64 - 1);
-    r.a = x - a + (wave ? lane_value(p, wave - 1) : 0u);
-    r.b = y - b + (wave ? lane_value(q, wave - 1) : 0u);
-    __syncthreads();
-    return r;
+    const uint32_t p = wave_scan(lane < PARTS ? waves[lane % PARTS] : 0u);     // every wavefront scans the wavefronts' totals itself
+    return x - a + (wave ? lane_value(p, wave - 1) : 0u);
 }
 
-// HELD: quads of weights that a thread keeps in registers (4 HELD neighbouring slots, all of a list in 4096 HELD slots); 0: the list
-// is read again for each pass, 4096 slots at a time.  8000 slots, 320 lists: 20.4 us when every list was read four times.
+// HELD: quads of weights that a thread keeps in registers, every 4096 slots one (all of a list in 4096 HELD slots); 0: the list is read
+// again for each pass, 4096 slots at a time.  8000 slots, 320 lists: 20.4 us when every list was read four times.  60000 slots, 20 lists:
+// 40 us when a thread had 64 neighbouring slots.
 // WHOLE: rows of weights start on 16 bytes.
 template <int HELD, bool WHOLE>
 __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a) {
     // Weights crowd into few bins of the first pass (their exponents): eight copies of each bin, side by side in neighbouring
     // banks, so that a wavefront's lanes do not queue for one address.
     __shared__ __attribute__((aligned(16))) uint32_t hist[SEL_BINS * SEL_COPIES];
-    __shared__ uint2 waves[SEL_THREADS / 64];
+    __shared__ uint32_t waves[PARTS];
     __shared__ uint32_t s_bin, s_above;
-    constexpr int Q = HELD ? HELD : 1;
+    constexpr int Q = HELD ? HELD : 1, STEP = 4 * SEL_THREADS;
     const int b = blockIdx.x / a.n_kv, tid = threadIdx.x;
     const int len = clampi(a.lens[b], 0, a.max_len);
     int32_t* kept = a.kept + (size_t)blockIdx.x * a.keep;
@@ -212,24 +202,30 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
     uint32_t key[4 * Q];                              // 0 (below every key of a weight) outside lo .. hi - 1
     // (loads past the list read its row's end, not used: a load that might not happen is waited for before the next)
     const int row_end = a.ld < (size_t)hi + 3 ? (int)a.ld : hi + 3;
-    auto read = [&](int i0) {
+    auto read = [&](int i0) {                         // quads 4096 slots apart
         if constexpr (WHOLE) {
 #pragma unroll
             for (int j = 0; j < Q; ++j) {
-                const int i = i0 + 4 * j, at = i + 4 <= row_end ? i : (row_end & ~3) - 4;
+                const int i = i0 + j * STEP, at = i + 4 <= row_end ? i : (row_end & ~3) - 4;
                 const float4 x = *reinterpret_cast<const float4*>(w + (at < 0 ? 0 : at));
                 key[4 * j] = __float_as_uint(x.x); key[4 * j + 1] = __float_as_uint(x.y);
                 key[4 * j + 2] = __float_as_uint(x.z); key[4 * j + 3] = __float_as_uint(x.w);
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < 4 * Q; ++e) key[e] = __float_as_uint(w[i0 + e < hi ? i0 + e : hi - 1]);
+            for (int e = 0; e < 4 * Q; ++e) {
+                const int i = i0 + e / 4 * STEP + e % 4;
+                key[e] = __float_as_uint(w[i < hi ? i : hi - 1]);
+            }
         }
 #pragma unroll
-        for (int e = 0; e < 4 * Q; ++e) key[e] = weight_key(__uint_as_float(key[e])) & ((unsigned)(i0 + e - lo) < (unsigned)(hi - lo) ? ~0u : 0u);
+        for (int e = 0; e < 4 * Q; ++e) {
+            const int i = i0 + e / 4 * STEP + e % 4;
+            key[e] = weight_key(__uint_as_float(key[e])) & ((unsigned)(i - lo) < (unsigned)(hi - lo) ? ~0u : 0u);
+        }
     };
-    const int steps = HELD ? 1 : (hi + 4 * SEL_THREADS - 1) / (4 * SEL_THREADS);
-    if (HELD) read(tid * 4 * Q);
+    const int steps = HELD ? 1 : (hi + STEP - 1) / STEP;
+    if (HELD) read(tid * 4);
     for (int i = tid; i < a.first; i += SEL_THREADS) kept[i] = i;
     for (int i = tid; i < a.recent; i += SEL_THREADS) kept[a.first + mid + i] = hi + i;
     if (mid == 0) return;
@@ -241,7 +237,7 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
         for (int i = tid; i < SEL_BINS * SEL_COPIES / 4; i += SEL_THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
         for (int step = 0; step < steps; ++step) {
-            if (!HELD) read((step * SEL_THREADS + tid) * 4);
+            if (!HELD) read(step * STEP + tid * 4);
 #pragma unroll
             for (int e = 0; e < 4 * Q; ++e) {
                 if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
@@ -257,36 +253,67 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
             return x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
         };
         const uint32_t h0 = in_bin(b0), h1 = in_bin(b1);
-        const uint32_t before = scan_before(h0 + h1, 0u, waves).a;
+        const uint32_t before = scan_before(h0 + h1, waves);
         if (before < want && want <= before + h0) { s_bin = b0; s_above = before; }
         else if (before + h0 < want && want <= before + h0 + h1) { s_bin = b1; s_above = before + h0; }
         __syncthreads();
         prefix = (prefix << bits) | s_bin;
         want -= s_above;
     }
-    // in slot order: all above the threshold, the first `want` equal to it
+    // in slot order: all above the threshold, the first `want` equal to it.  What lies in front of a quad: in its wavefront's part of the
+    // step (above | equal << 16), in front of that part.
+    __shared__ uint32_t part[Q * PARTS];
+    __shared__ uint2 front[Q * PARTS];
+    const int lane = tid & 63, wave = tid >> 6;
     uint32_t greater = 0, equal = 0;                  // in front of the step
     for (int step = 0; step < steps; ++step) {
-        const int i0 = HELD ? tid * 4 * Q : (step * SEL_THREADS + tid) * 4;
+        const int i0 = step * STEP + tid * 4;
         if (!HELD) read(i0);
-        uint32_t g = 0, q = 0;
+        uint32_t mine[Q];
 #pragma unroll
-        for (int e = 0; e < 4 * Q; ++e) {
-            g += key[e] > prefix;
-            q += key[e] == prefix;
-        }
-        const Before s = scan_before(g, q, waves);
-        uint32_t gb = greater + s.a, qb = equal + s.b;
+        for (int j = 0; j < Q; ++j) {
+            uint32_t n = 0;
 #pragma unroll
-        for (int e = 0; e < 4 * Q; ++e) {
-            if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-            const bool over = key[e] > prefix, same = key[e] == prefix;
-            if (over || (same && qb < want)) kept[a.first + gb + (qb < want ? qb : want)] = i0 + e;
-            gb += over;
-            qb += same;
+            for (int e = 4 * j; e < 4 * j + 4; ++e) n += key[e] > prefix ? 1u : key[e] == prefix ? 0x10000u : 0u;
+            const uint32_t x = wave_scan(n);
+            if (lane == 63) part[j * PARTS + wave] = x;
+            mine[j] = x - n;
         }
-        greater += s.all_a;
-        equal += s.all_b;
+        __syncthreads();
+        uint32_t all_g, all_q;
+        if (wave == 0) {
+            constexpr int PER = (Q * PARTS + 63) / 64;
+            uint32_t g[PER], q[PER], sum_g = 0, sum_q = 0;
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                const uint32_t n = lane * PER + x < Q * PARTS ? part[lane * PER + x] : 0u;
+                g[x] = n & 0xffffu; q[x] = n >> 16;
+                sum_g += g[x]; sum_q += q[x];
+            }
+            uint32_t at_g = wave_scan(sum_g), at_q = wave_scan(sum_q);
+            all_g = lane_value(at_g, 63); all_q = lane_value(at_q, 63);
+            at_g -= sum_g; at_q -= sum_q;
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                if (lane * PER + x < Q * PARTS) front[lane * PER + x] = make_uint2(greater + at_g, equal + at_q);
+                at_g += g[x]; at_q += q[x];
+            }
+            greater += all_g;                         // (of wavefront 0, which counts on)
+            equal += all_q;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < Q; ++j) {
+            const uint2 f = front[j * PARTS + wave];
+            uint32_t gb = f.x + (mine[j] & 0xffffu), qb = f.y + (mine[j] >> 16);
+#pragma unroll
+            for (int e = 4 * j; e < 4 * j + 4; ++e) {
+                const bool over = key[e] > prefix, same = key[e] == prefix;
+                if (over || (same && qb < want)) kept[a.first + gb + (qb < want ? qb : want)] = i0 + j * STEP + e % 4;
+                gb += over;
+                qb += same;
+            }
+        }
     }
 }
 
