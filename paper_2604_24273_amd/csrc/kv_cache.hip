@@ -178,13 +178,14 @@ __device__ __forceinline__ uint32_t scan_before(uint32_t a, uint32_t* waves) {
 
 // HELD: quads of weights that a thread keeps in registers, every 4096 slots one (all of a list in 4096 HELD slots); 0: the list is read
 // again for each pass, 4096 slots at a time.  8000 slots, 320 lists: 20.4 us when every list was read four times.  60000 slots, 20 lists:
-// 40 us when a thread had 64 neighbouring slots.
+// 40 us when a thread had 64 neighbouring slots, 28 now.
 // WHOLE: rows of weights start on 16 bytes.
 template <int HELD, bool WHOLE>
 __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a) {
-    // Weights crowd into few bins of the first pass (their exponents): eight copies of each bin, side by side in neighbouring
-    // banks, so that a wavefront's lanes do not queue for one address.
-    __shared__ __attribute__((aligned(16))) uint32_t hist[SEL_BINS * SEL_COPIES];
+    // Weights crowd into few bins of the first pass (their exponents): copies of each bin, side by side in neighbouring banks, so that a
+    // wavefront's lanes do not queue for one address.
+    constexpr int COPIES = HELD > 4 ? 16 : 8;         // (a list of many slots has the compute unit to itself)
+    __shared__ __attribute__((aligned(16))) uint32_t hist[SEL_BINS * COPIES];
     __shared__ uint32_t waves[PARTS];
     __shared__ uint32_t s_bin, s_above;
     constexpr int Q = HELD ? HELD : 1, STEP = 4 * SEL_THREADS;
@@ -226,55 +227,77 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
     };
     const int steps = HELD ? 1 : (hi + STEP - 1) / STEP;
     if (HELD) read(tid * 4);
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    auto quads = [&](int step) {                      // of this wavefront that hold any slot of the list
+        const int n = (hi - step * STEP - wave * 256 + STEP - 1) / STEP;
+        return n < Q ? n : Q;
+    };
     for (int i = tid; i < a.first; i += SEL_THREADS) kept[i] = i;
     for (int i = tid; i < a.recent; i += SEL_THREADS) kept[a.first + mid + i] = hi + i;
     if (mid == 0) return;
     uint32_t prefix = 0, want = mid;                  // still to be taken among the keys that begin with prefix
-    int shift = 32;
-    for (int pass = 0; pass < 3; ++pass) {
-        const int bits = pass < 2 ? 11 : 10, above = shift;
-        shift -= bits;
-        for (int i = tid; i < SEL_BINS * SEL_COPIES / 4; i += SEL_THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+    auto pass = [&](auto number) __attribute__((always_inline)) {
+        constexpr int P = decltype(number)::value, BITS = P < 2 ? 11 : 10, SHIFT = P == 0 ? 21 : P == 1 ? 10 : 0;
+        for (int i = tid; i < SEL_BINS * COPIES / 4; i += SEL_THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
+        uint32_t* const mine = hist + tid % COPIES;
         for (int step = 0; step < steps; ++step) {
             if (!HELD) read(step * STEP + tid * 4);
+            const int n = quads(step);
 #pragma unroll
-            for (int e = 0; e < 4 * Q; ++e) {
-                if (e % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-                if (key[e] && (pass == 0 || key[e] >> above == prefix)) atomicAdd(&hist[((key[e] >> shift) & ((1u << bits) - 1)) * SEL_COPIES + tid % SEL_COPIES], 1u);
+            for (int j = 0; j < Q; ++j) {
+                if (j >= n) continue;                 // (a loop with an end of its own would have the keys in memory)
+#pragma unroll
+                for (int e = 4 * j; e < 4 * j + 4; ++e) {
+                    // (0, no slot's key, falls into bin 0 of the first pass, far below the threshold: -inf is in bin 3)
+                    const bool in = P == 0 || key[e] - (prefix << (SHIFT + BITS & 31)) < (1u << (SHIFT + BITS & 31));
+                    if (in) atomicAdd(mine + (key[e] >> SHIFT & ((1u << BITS) - 1)) * COPIES, 1u);
+                }
             }
         }
         __syncthreads();
         // bins from the top: thread t has bins top - 2 t and top - 2 t - 1
-        const int top = (1 << bits) - 1, b0 = top - 2 * tid, b1 = b0 - 1;
+        const int top = (1 << BITS) - 1, b0 = top - 2 * tid, b1 = b0 - 1;
         auto in_bin = [&](int i) {
-            if (i < 0) return 0u;
-            const uint4 x = reinterpret_cast<const uint4*>(hist)[2 * i], y = reinterpret_cast<const uint4*>(hist)[2 * i + 1];
-            return x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+            uint32_t n = 0;
+            if (i < 0) return n;
+#pragma unroll
+            for (int x = 0; x < COPIES / 4; ++x) {
+                const uint4 f = reinterpret_cast<const uint4*>(hist)[COPIES / 4 * i + x];
+                n += f.x + f.y + f.z + f.w;
+            }
+            return n;
         };
         const uint32_t h0 = in_bin(b0), h1 = in_bin(b1);
         const uint32_t before = scan_before(h0 + h1, waves);
         if (before < want && want <= before + h0) { s_bin = b0; s_above = before; }
         else if (before + h0 < want && want <= before + h0 + h1) { s_bin = b1; s_above = before + h0; }
         __syncthreads();
-        prefix = (prefix << bits) | s_bin;
+        prefix = (prefix << BITS) | s_bin;
         want -= s_above;
-    }
+    };
+    pass(std::integral_constant<int, 0>());
+    pass(std::integral_constant<int, 1>());
+    pass(std::integral_constant<int, 2>());
     // in slot order: all above the threshold, the first `want` equal to it.  What lies in front of a quad: in its wavefront's part of the
     // step (above | equal << 16), in front of that part.
     __shared__ uint32_t part[Q * PARTS];
     __shared__ uint2 front[Q * PARTS];
-    const int lane = tid & 63, wave = tid >> 6;
     uint32_t greater = 0, equal = 0;                  // in front of the step
     for (int step = 0; step < steps; ++step) {
-        const int i0 = step * STEP + tid * 4;
+        int i0 = step * STEP + tid * 4;
         if (!HELD) read(i0);
+        asm volatile("" : "+v"(i0));                  // (opaque: or all slots' numbers are kept in registers from the first read on)
         uint32_t mine[Q];
 #pragma unroll
         for (int j = 0; j < Q; ++j) {
-            uint32_t n = 0;
+            uint32_t over = 0, least = 0;             // above the threshold; not below it
 #pragma unroll
-            for (int e = 4 * j; e < 4 * j + 4; ++e) n += key[e] > prefix ? 1u : key[e] == prefix ? 0x10000u : 0u;
+            for (int e = 4 * j; e < 4 * j + 4; ++e) {
+                over += key[e] > prefix;
+                least += key[e] >= prefix;
+            }
+            const uint32_t n = over | (least - over) << 16;
             const uint32_t x = wave_scan(n);
             if (lane == 63) part[j * PARTS + wave] = x;
             mine[j] = x - n;
@@ -305,12 +328,13 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
 #pragma unroll
         for (int j = 0; j < Q; ++j) {
             const uint2 f = front[j * PARTS + wave];
-            uint32_t gb = f.x + (mine[j] & 0xffffu), qb = f.y + (mine[j] >> 16);
+            uint32_t qb = f.y + (mine[j] >> 16);
+            uint32_t at = (a.first + f.x + (mine[j] & 0xffffu) + (qb < want ? qb : want)) * 4;        // (bytes: keep is below 2^28)
 #pragma unroll
             for (int e = 4 * j; e < 4 * j + 4; ++e) {
-                const bool over = key[e] > prefix, same = key[e] == prefix;
-                if (over || (same && qb < want)) kept[a.first + gb + (qb < want ? qb : want)] = i0 + j * STEP + e % 4;
-                gb += over;
+                const bool same = key[e] == prefix, take = key[e] > prefix || (same && qb < want);
+                if (take) *reinterpret_cast<int32_t*>(reinterpret_cast<char*>(kept) + at) = i0 + j * STEP + e % 4;
+                at += take ? 4u : 0u;
                 qb += same;
             }
         }
