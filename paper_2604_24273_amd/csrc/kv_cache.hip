@@ -1,4 +1,6 @@
 // The paged key/value cache apart from attention: storing new tokens, choosing which slots to keep, moving them together.
+#include <type_traits>
+
 #include "common.hpp"
 
 namespace brl {
@@ -203,7 +205,13 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
     uint32_t key[4 * Q];                              // 0 (below every key of a weight) outside lo .. hi - 1
     // (loads past the list read its row's end, not used: a load that might not happen is waited for before the next)
     const int row_end = a.ld < (size_t)hi + 3 ? (int)a.ld : hi + 3;
-    auto read = [&](int i0) {                         // quads 4096 slots apart
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    auto quads = [&](int step) {                      // how many of this wavefront's hold any slot of the list
+        const int n = (hi - step * STEP - wave * 256 + STEP - 1) / STEP;
+        return n < Q ? n : Q;
+    };
+    auto read = [&](int step) {                       // quads 4096 slots apart
+        const int i0 = step * STEP + tid * 4;
         if constexpr (WHOLE) {
 #pragma unroll
             for (int j = 0; j < Q; ++j) {
@@ -219,19 +227,19 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
                 key[e] = __float_as_uint(w[i < hi ? i : hi - 1]);
             }
         }
+        const int n = quads(step);
 #pragma unroll
-        for (int e = 0; e < 4 * Q; ++e) {
-            const int i = i0 + e / 4 * STEP + e % 4;
-            key[e] = weight_key(__uint_as_float(key[e])) & ((unsigned)(i - lo) < (unsigned)(hi - lo) ? ~0u : 0u);
+        for (int j = 0; j < Q; ++j) {
+            if (j >= n) continue;                     // (its keys are not looked at)
+#pragma unroll
+            for (int e = 4 * j; e < 4 * j + 4; ++e) {
+                const int i = i0 + j * STEP + e % 4;
+                key[e] = weight_key(__uint_as_float(key[e])) & ((unsigned)(i - lo) < (unsigned)(hi - lo) ? ~0u : 0u);
+            }
         }
     };
     const int steps = HELD ? 1 : (hi + STEP - 1) / STEP;
-    if (HELD) read(tid * 4);
-    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    auto quads = [&](int step) {                      // of this wavefront that hold any slot of the list
-        const int n = (hi - step * STEP - wave * 256 + STEP - 1) / STEP;
-        return n < Q ? n : Q;
-    };
+    if (HELD) read(0);
     for (int i = tid; i < a.first; i += SEL_THREADS) kept[i] = i;
     for (int i = tid; i < a.recent; i += SEL_THREADS) kept[a.first + mid + i] = hi + i;
     if (mid == 0) return;
@@ -242,7 +250,7 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
         __syncthreads();
         uint32_t* const mine = hist + tid % COPIES;
         for (int step = 0; step < steps; ++step) {
-            if (!HELD) read(step * STEP + tid * 4);
+            if (!HELD) read(step);
             const int n = quads(step);
 #pragma unroll
             for (int j = 0; j < Q; ++j) {
@@ -288,11 +296,17 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
     uint32_t greater = 0, equal = 0;                  // in front of the step
     for (int step = 0; step < steps; ++step) {
         int i0 = step * STEP + tid * 4;
-        if (!HELD) read(i0);
+        if (!HELD) read(step);
         asm volatile("" : "+v"(i0));                  // (opaque: or all slots' numbers are kept in registers from the first read on)
         uint32_t mine[Q];
+        const int live = quads(step);
 #pragma unroll
         for (int j = 0; j < Q; ++j) {
+            mine[j] = 0;
+            if (j >= live) {
+                if (lane == 0) part[j * PARTS + wave] = 0;
+                continue;
+            }
             uint32_t over = 0, least = 0;             // above the threshold; not below it
 #pragma unroll
             for (int e = 4 * j; e < 4 * j + 4; ++e) {
@@ -333,6 +347,7 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
             asm volatile("" : "+v"(i0));              // (opaque: see above)
 #pragma unroll
             for (int j = 0; j < Q; ++j) {
+                if (j >= live) continue;
                 const uint2 f = front[j * PARTS + wave];
                 uint32_t qb = f.y + (mine[j] >> 16);
                 uint32_t at = f.x + (mine[j] & 0xffffu) + (qb < want ? qb : want) - from;
