@@ -378,7 +378,7 @@ __global__ __launch_bounds__(SEL_THREADS) void cache_select_kernel(SelectArgs a)
 // head and walks them in ascending order, a chunk at a time: what a chunk overwrites lies below the sources of every later
 // chunk, so the only order needed is that all of a chunk has been read before any of it is written.  While a chunk's rows are
 // on their way the places of the next chunk's are looked up (list, then page table).
-constexpr int CP_THREADS = 256, CP_ITEMS = 8, CP_INFLIGHT = CP_THREADS * CP_ITEMS;
+constexpr int CP_ITEMS = 8;                           // sixteen bytes of a thread in a chunk
 
 typedef uint32_t chunk16 __attribute__((ext_vector_type(4)));
 
@@ -399,11 +399,12 @@ struct Move {
 };
 
 // units `first` .. first + units - 1 of every row, rows of `row_units` units of type T
-template <class T>
+template <int THREADS, class T>
 __device__ __forceinline__ void move_rows(const Move& m, T* pool, int row_units, int first, int units, int2* places) {
-    const int rows = CP_INFLIGHT / units;             // of a chunk
-    const int tid = threadIdx.x, q = CP_THREADS / units, rem = CP_THREADS % units;
-    for (int i = tid; i < rows; i += CP_THREADS) places[i] = m.place(i);
+    constexpr int INFLIGHT = THREADS * CP_ITEMS;
+    const int rows = INFLIGHT / units;             // of a chunk
+    const int tid = threadIdx.x, q = THREADS / units, rem = THREADS % units;
+    for (int i = tid; i < rows; i += THREADS) places[i] = m.place(i);
     __syncthreads();
     int buf = 0;
     for (int r0 = 0; r0 < m.count; r0 += rows) {
@@ -414,7 +415,7 @@ __device__ __forceinline__ void move_rows(const Move& m, T* pool, int row_units,
 #pragma unroll
         for (int e = 0; e < CP_ITEMS; ++e) {
             // (what does not move reads row 0: loads that might not happen would each be waited for)
-            const int2 x = r < rows ? places[buf * CP_INFLIGHT + r] : make_int2(-1, -1);
+            const int2 x = r < rows ? places[buf * INFLIGHT + r] : make_int2(-1, -1);
             moves[e] = x.x >= 0;
             v[e] = pool[(size_t)(moves[e] ? x.x : 0) * row_units + first + u];
             to[e] = (size_t)(moves[e] ? x.y : 0) * row_units + first + u;
@@ -427,7 +428,7 @@ __device__ __forceinline__ void move_rows(const Move& m, T* pool, int row_units,
         }
         buf ^= 1;
         if (r0 + rows < m.count)
-            for (int i = tid; i < rows; i += CP_THREADS) places[buf * CP_INFLIGHT + i] = m.place(r0 + rows + i);
+            for (int i = tid; i < rows; i += THREADS) places[buf * INFLIGHT + i] = m.place(r0 + rows + i);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // read, not only requested
         __syncthreads();
 #pragma unroll
@@ -437,26 +438,43 @@ __device__ __forceinline__ void move_rows(const Move& m, T* pool, int row_units,
     __syncthreads();
 }
 
-__global__ __launch_bounds__(CP_THREADS) void cache_compact_kernel(CompactArgs a, int slices, int units, int row_units) {
-    __shared__ int2 places[2 * CP_INFLIGHT];
-    const int parts = 2 * slices + 1;
-    const int part = blockIdx.x % parts, h = blockIdx.x / parts % a.c.n_kv, b = blockIdx.x / (parts * a.c.n_kv);
+// How a row of k or v is cut into slices of `units` times 16 bytes.  Slices that share 128 bytes (`near` of them) are workgroups whose
+// numbers differ by multiples of 8: they run on one die, whose L2 so fetches the line once.
+struct Slices {
+    int units, row_units, count, near, lines;         // lines: of a row, count / near rounded up
+    int main_blocks;                                  // workgroups for k and v; behind them one per list for scales and weights
+};
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void cache_compact_kernel(CompactArgs a, Slices sl) {
+    __shared__ int2 places[2 * THREADS * CP_ITEMS];
+    int list, slice = 0, line = 0;
+    const bool rows = blockIdx.x < (unsigned)sl.main_blocks;
+    if (rows) {
+        const int many = 8 * sl.near, r = blockIdx.x % many;
+        line = blockIdx.x / many * 8 + r % 8;         // of all lists' keys and values
+        list = line / (2 * sl.lines);
+        slice = line % sl.lines * sl.near + r / 8;
+        if (list >= a.B * a.c.n_kv || slice >= sl.count) return;
+    } else {
+        list = blockIdx.x - sl.main_blocks;
+    }
+    const int h = list % a.c.n_kv, b = list / a.c.n_kv;
     const int len = clampi(a.lens[b], 0, a.max_len);
     const int start = a.start ? clampi(a.start[b], 0, len) : 0;
     const int most = len - start < a.ld_kept ? len - start : a.ld_kept;
     Move m = {a, a.kept + ((size_t)b * a.kept_heads + (a.kept_heads == 1 ? 0 : h)) * a.ld_kept, b, h, len, start, clampi(a.counts[b], 0, most), true};
-    if (part < 2 * slices) {
-        const int first = part % slices * units;
-        move_rows(m, reinterpret_cast<chunk16*>(part < slices ? a.c.k : a.c.v), row_units, first,
-                  row_units - first < units ? row_units - first : units, places);
+    if (rows) {
+        const int first = slice * sl.units;
+        move_rows<THREADS>(m, reinterpret_cast<chunk16*>(line / sl.lines % 2 ? a.c.v : a.c.k), sl.row_units, first,
+                  sl.row_units - first < sl.units ? sl.row_units - first : sl.units, places);
         return;
     }
     if (a.c.dtype == BRL_I8) {
-        move_rows(m, a.c.ks, 1, 0, 1, places);
-        move_rows(m, a.c.vs, 1, 0, 1, places);
+        move_rows<THREADS>(m, a.c.ks, 1, 0, 1, places);
+        move_rows<THREADS>(m, a.c.vs, 1, 0, 1, places);
     }
     m.paged = false;
-    if (a.weights) move_rows(m, a.weights + ((size_t)b * a.c.n_kv + h) * a.ld_weights, 1, 0, 1, places);
+    if (a.weights) move_rows<THREADS>(m, a.weights + ((size_t)b * a.c.n_kv + h) * a.ld_weights, 1, 0, 1, places);
 }
 
 }  // namespace
@@ -493,14 +511,25 @@ int launch_cache_select(const float* weights, size_t ld_weights, int B, int n_kv
 
 int launch_cache_compact(const CompactArgs& a, hipStream_t s) {
     const int row_units = a.c.row * kv_bytes(a.c.dtype) / 16;
-    // Whole rows where the heads alone fill the chip; narrower slices, down to 32 bytes, where there are few of them.
+    // A workgroup has 8 x 16 bytes per thread under way and pays a chunk's way from memory each time (5 us): where lists are few they take
+    // 1024 threads, which fill a compute unit, and rows are cut, down to 32 bytes, into as many slices as there are units.  Keys and values
+    // of fp16, us with 256 threads and up to 512 workgroups / so: 20 lists of 7000 slots 69 / 48, 6 heads of 64, 24000 slots 92 / 58,
+    // 65 of 1000 19 / 18; fp32, 50 of 11000 173 / 160.  More than 256 workgroups: 205 lists of 500 slots 18 / 24.
     int slices = 1;
-    while ((long long)a.B * a.c.n_kv * 2 * slices < 512 && row_units / (2 * slices) >= 2) slices *= 2;
-    const int units = (row_units + slices - 1) / slices;
-    slices = (row_units + units - 1) / units;
+    while ((long long)a.B * a.c.n_kv * 4 * slices <= 256 && row_units / (2 * slices) >= 2) slices *= 2;
+    Slices sl;
+    sl.row_units = row_units;
+    sl.units = (row_units + slices - 1) / slices;
+    sl.count = (row_units + sl.units - 1) / sl.units;
+    sl.near = sl.units >= 8 ? 1 : 8 / sl.units < sl.count ? 8 / sl.units : sl.count;
+    sl.lines = (sl.count + sl.near - 1) / sl.near;
+    sl.main_blocks = (a.B * a.c.n_kv * 2 * sl.lines + 7) / 8 * 8 * sl.near;
+    const int others = a.c.dtype == BRL_I8 || a.weights ? a.B * a.c.n_kv : 0;
     LaunchTimer tm(BRL_KC_ATTENTION, s);
-    hipLaunchKernelGGL(cache_compact_kernel, dim3((unsigned)(a.B * a.c.n_kv * (2 * slices + 1))), dim3(CP_THREADS), 0, s, a, slices, units,
-                       row_units);
+    const dim3 grid((unsigned)(sl.main_blocks + others));
+    const bool large = (long long)a.B * a.c.n_kv * 2 * sl.count <= 256 && a.ld_kept > 256 * CP_ITEMS / sl.units;      // (and several chunks)
+    if (large) hipLaunchKernelGGL(cache_compact_kernel<1024>, grid, dim3(1024), 0, s, a, sl);
+    else hipLaunchKernelGGL(cache_compact_kernel<256>, grid, dim3(256), 0, s, a, sl);
     BRL_LAUNCH_CHECK("cache_compact_kernel");
     return BRL_OK;
 }
