@@ -381,6 +381,10 @@ int attention_forward(const float* qkv, int B, int S,
  * moved), a token that has no slot (more new tokens than lens) sees no key
  * before slot 0 and is not stored.
  * All calls only enqueue kernels and can be captured into a HIP graph.
+ * BRL_EINVAL where one call would be too much: B n_heads above 2^22, max_new
+ * n_heads B above 2^26, max_new times the square of the heads per k/v head from
+ * 2^32 on, B n_kv_heads max_len above 2^30 with weights, B n_kv_heads above 2^21
+ * (select) or 2^18 (compact).
  *
  * attention_cache_append: rotates the new keys, stores keys and values.
  *   fp16: rounded to nearest (|x| < 65504).  int8, per row: a = max(max|x|,
@@ -394,9 +398,10 @@ int attention_forward(const float* qkv, int B, int S,
  *   new tokens, and the state's new token j where bit j % 32 of word j / 32 is
  *   set (a set bit for itself and for its ancestors: candidate texts as branches of one
  *   prefix, evaluated together); tokens from 32 * mask_words on are not seen.
- *   A token that sees nothing gives zeros.  The cache's values within
- *   |x| < 65504 (BRL_F32: fp16 hi + lo pairs on the matrix cores, as in
- *   BRL_ATTN_MFMA).  What is infinite or NaN in a slot reaches the tokens that see
+ *   A token that sees nothing gives zeros.  Queries and the cache's values within
+ *   |x| < 65504 (on the matrix cores queries and BRL_F32 rows are fp16 hi + lo
+ *   pairs, as in BRL_ATTN_MFMA: a number is carried to 2^-22 of itself or to 3e-8,
+ *   whichever is more).  What is infinite or NaN in a slot reaches the tokens that see
  *   the slot and no others.
  *   weights, DEVICE [B, n_kv_heads, ld_weights] or NULL: weights[b, h, j] += sum
  *   over the state's new tokens and the query heads of k/v head h of the softmax

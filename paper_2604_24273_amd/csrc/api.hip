@@ -984,6 +984,7 @@ int view_cache(const brl_kv_cache* c, const char* who, KvView& v) {
     BRL_REQUIRE(c->k && c->v && c->page_table && aligned16(c->k) && aligned16(c->v), "%s: null or misaligned pointer in brl_kv_cache", who);
     BRL_REQUIRE((c->dtype == BRL_I8) == (c->k_scale != nullptr) && (c->dtype == BRL_I8) == (c->v_scale != nullptr),
                 "%s: an int8 cache needs k_scale and v_scale, any other has none", who);
+    BRL_REQUIRE(aligned16(c->k_scale) && aligned16(c->v_scale), "%s: misaligned k_scale or v_scale", who);
     v.k = static_cast<char*>(c->k); v.v = static_cast<char*>(c->v);
     v.ks = c->k_scale; v.vs = c->v_scale;
     v.table = c->page_table;
@@ -995,6 +996,13 @@ int view_cache(const brl_kv_cache* c, const char* who, KvView& v) {
 
 bool head_counts_ok(int n_heads, int n_kv_heads) { return n_heads >= n_kv_heads && n_heads <= 4096 && n_heads % n_kv_heads == 0; }
 
+// Workgroups and items of a launch are counted in 32 bits; rows are divided by the group by a 32-bit multiplication.
+bool one_call(long long max_new, int B, int n_heads, int n_kv_heads) {
+    const long long group = n_heads / n_kv_heads;
+    return (long long)B * n_heads <= (1 << 22) && max_new * n_heads * B <= (1ll << 26) && max_new * group * group < (1ll << 32);
+}
+constexpr long long KV_MAX_WEIGHTS = 1ll << 30;      // of a call: B n_kv_heads max_len
+
 int check_new_tokens(const KvView& v, const float* qkv, int n_heads, int T, int B, const int32_t* cu_new, int max_new, const int32_t* lens,
                      const int32_t* positions, const float* rope_cos, const float* rope_sin, int rope_len, const char* who, NewTokens& t) {
     BRL_REQUIRE(qkv && lens && rope_cos && rope_sin && aligned16(qkv) && aligned16(rope_cos) && aligned16(rope_sin),
@@ -1005,10 +1013,7 @@ int check_new_tokens(const KvView& v, const float* qkv, int n_heads, int T, int 
                 who, T, B, max_new);
     BRL_REQUIRE(rope_len >= 1, "%s: rope_len = %d", who, rope_len);
     if (max_new > T) max_new = T;
-    // workgroups and items of a launch are counted in 32 bits
-    BRL_REQUIRE((long long)max_new * n_heads * B <= (1ll << 26) && (long long)B * n_heads <= (1 << 22) &&
-                    (long long)max_new * (n_heads / v.n_kv) * (n_heads / v.n_kv) < (1ll << 32),
-                "%s: too much for one call (max_new %d, B %d, n_heads %d)", who, max_new, B, n_heads);
+    BRL_REQUIRE(one_call(max_new, B, n_heads, v.n_kv), "%s: too much for one call (max_new %d, B %d, n_heads %d)", who, max_new, B, n_heads);
     t.cu = cu_new; t.lens = lens; t.pos = positions;
     t.cos_t = rope_cos; t.sin_t = rope_sin;
     t.T = T; t.B = B; t.max_new = max_new; t.max_len = v.table_pages << v.page_shift; t.rope_len = rope_len;
@@ -1047,6 +1052,7 @@ size_t brl_attention_cached_workspace_bytes(const brl_kv_cache* c, int n_heads, 
         T > KV_MAX_TOKENS || B < 1 || max_new < 1 || max_len < 1 || max_len > KV_MAX_TOKENS)
         return 0;
     if (max_new > T) max_new = T;
+    if (!one_call(max_new, B, n_heads, c->n_kv_heads) || (want_weights && (long long)B * c->n_kv_heads * max_len > KV_MAX_WEIGHTS)) return 0;
     KvView v;
     memset(&v, 0, sizeof(v));
     v.n_kv = c->n_kv_heads; v.dh = c->head_dim; v.row = kv_row(c->head_dim); v.dtype = c->dtype;
@@ -1068,7 +1074,7 @@ int attention_cached_forward(const brl_kv_cache* cache, const float* qkv, int n_
     BRL_REQUIRE((tree_mask == nullptr) == (mask_words == 0) && mask_words >= 0 && mask_words <= KV_MAX_TOKENS / 32,
                 "%s: mask_words = %d", who, mask_words);
     BRL_REQUIRE(!weights || ld_weights >= max_len, "%s: ld_weights = %d below max_len = %d", who, ld_weights, max_len);
-    BRL_REQUIRE(!weights || (long long)B * a.c.n_kv * max_len <= (1ll << 30), "%s: too many weights for one call (B %d, n_kv_heads %d, max_len %d)",
+    BRL_REQUIRE(!weights || (long long)B * a.c.n_kv * max_len <= KV_MAX_WEIGHTS, "%s: too many weights for one call (B %d, n_kv_heads %d, max_len %d)",
                 who, B, a.c.n_kv, max_len);
     const size_t need = brl_attention_cached_workspace_bytes(cache, n_heads, T, B, max_new, max_len, weights != nullptr);
     if (ws_bytes < need) {

@@ -52,7 +52,8 @@ def test_caches_are_checked(B):
                       (dict(n_pages=0), "n_pages"), (dict(table_pages=0), "table_pages"), (dict(table_pages=1 << 30), "table_pages"),
                       (dict(n_pages=2 ** 25), "rows"), (dict(k=None), "null"), (dict(v=ODD), "misaligned"), (dict(page_table=None), "null"),
                       (dict(dtype=B.BRL_I8), "k_scale"), (dict(k_scale=FAKE), "k_scale"),
-                      (dict(dtype=B.BRL_I8, k_scale=FAKE), "v_scale")):
+                      (dict(dtype=B.BRL_I8, k_scale=FAKE), "v_scale"), (dict(dtype=B.BRL_I8, k_scale=ODD, v_scale=FAKE), "k_scale"),
+                      (dict(dtype=B.BRL_I8, k_scale=FAKE, v_scale=ODD), "v_scale")):
         assert append(cache(B, **bad)) == B.BRL_EINVAL and word in err(), bad
     ok = cache(B)
     for bad, word in ((dict(hq=3), "n_heads"), (dict(hq=0), "n_heads"), (dict(T=0), "T = 0"), (dict(states=0), "B = 0"), (dict(max_new=0), "max_new"),
@@ -117,3 +118,26 @@ def test_struct_builder_checks_tensors(B):
         B.make_kv_cache(k, k, None, None, table.long(), 100)
     with pytest.raises(ValueError, match="GPU"):
         B.make_kv_cache(k, k, None, None, table, 100)
+
+
+def test_what_is_too_much_for_one_call(B):
+    lib = B.lib()
+    err = lambda: lib.brl_last_error().decode()  # noqa: E731
+    large = cache(B, n_kv_heads=1, table_pages=1 << 20)
+
+    def attend(hq, T, states, max_new, max_len=64, weights=None):
+        rc = lib.attention_cached_forward(C.byref(large), FAKE, hq, T, states, FAKE, max_new, FAKE, max_len, None, FAKE, FAKE, 16, None, 0,
+                                          FAKE, weights, max_len if weights else 0, FAKE, 0, None)
+        return rc, B.brl_attention_cached_workspace_bytes(large, hq, T, states, max_new, max_len, weights is not None)
+
+    # a workspace of 0 bytes is refused behind everything else
+    rc, need = attend(4096, 255, 1, 255)
+    assert rc == B.BRL_ENOSPC and need > 0
+    for call in ((4096, 256, 1, 256),                               # 256 tokens x 4096^2
+                 (4, 1 << 25, 1, 1 << 25), (4096, 1025, 1025, 1), (1, 1 << 23, 1 << 23, 1)):
+        rc, need = attend(*call)
+        assert rc == B.BRL_EINVAL and "too much" in err() and need == 0, call
+    rc, need = attend(1, 64, 64, 1, 1 << 24, FAKE)
+    assert rc == B.BRL_ENOSPC and need > 0
+    rc, need = attend(1, 65, 65, 1, 1 << 24, FAKE)
+    assert rc == B.BRL_EINVAL and "too many weights" in err() and need == 0
