@@ -547,6 +547,8 @@ struct Plan {
     float* lse;               // [B][n_kv][rows_pad] or nullptr: log2 of a row's sum, +inf where it sees nothing
     float* scores;            // few rows with weights: [B][n_kv][rows_max][ld_scores], else nullptr
     size_t ld_scores;
+    int w_parts;              // many rows with weights: parts of the rows whose sums are added up by a second kernel (1: none)
+    float* part_w;            // [w_parts][B][n_kv][ld_scores] or nullptr
 };
 
 __device__ __forceinline__ float* out_row(const CachedAttention& a, const StateTokens& st, int h, const Group& group, int r) {
@@ -1301,78 +1303,133 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
 }
 
 // Weights of slots, many rows: the scores once more.  A wavefront keeps a block of 32 keys in registers and walks the row tiles that
-// can see it; each lane sums its eight keys over its row of every tile, the sixteen rows meet at the end.
+// can see it (the next tile's queries on their way meanwhile); each lane sums its eight keys over its row of every tile, the sixteen rows
+// meet at the end.  Where blocks are few the row tiles go round among w_parts wavefronts.
+// Blocks per wavefront: every tile's queries come from the caches for each wavefront, 8 KB at heads of 128, so two where the keys' operands
+// leave the registers (80 heads, 2000 slots, 4000 rows, fp16: 970 us a call with two, 1250 with one).
+template <int DT>
+struct WeightBlocks {
+    static constexpr int N = DT == BRL_F32 ? 1 : 2;
+};
 template <int DT, int DH>
 __global__ __launch_bounds__(256, 2) void cached_tile_weights_kernel(CachedAttention a, Plan p, int chunks) {
     typedef Shape<DT, DH> S;
+    constexpr int NB = WeightBlocks<DT>::N;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-    const int unit = blockIdx.x / chunks, h = unit % a.c.n_kv, b = unit / a.c.n_kv;
+    const int units = a.t.B * a.c.n_kv, unit = blockIdx.x / chunks % units, part = blockIdx.x / chunks / units;
+    const int h = unit % a.c.n_kv, b = unit / a.c.n_kv;
     const StateTokens st = state_tokens(a.t, a.c, b);
-    const int rows = st.n * p.group.n, slot0 = (blockIdx.x % chunks * 4 + wave) * 32;
+    const int rows = st.n * p.group.n, slot0 = (blockIdx.x % chunks * 4 + wave) * 32 * NB;
     if (rows == 0 || slot0 >= st.len) return;
-    const int lo = kv_row_index(a.c, b, h, slot0), hi = slot0 + 16 < st.len ? kv_row_index(a.c, b, h, slot0 + 16) : -1;
-    const int n = st.len - slot0;
-    uint32_t there = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
-    if (lo < 0) there &= 0xffff0000u;
-    if (hi < 0) there &= 0x0000ffffu;
-    if (there == 0) return;
-    KeyLoads<S> raw;
-    raw.request(a.c.k, lo, hi, lane);
-    float kf[8];
-    if constexpr (DT == BRL_I8) {
+    v8h key[NB][2][S::KS][S::PL];
+    float kf[NB][8];
+    uint32_t mine[NB];                                                 // which of this lane's keys there are
 #pragma unroll
-        for (int e = 0; e < 8; ++e) kf[e] = a.c.ks[((e < 4 ? lo : hi) < 0 ? 0 : (e < 4 ? lo : hi)) + 4 * g + (e & 3)];
+    for (int n = 0; n < NB; ++n) {
+        const int slot = slot0 + 32 * n, left = st.len - slot;
+        const int lo = left > 0 ? kv_row_index(a.c, b, h, slot) : -1, hi = left > 16 ? kv_row_index(a.c, b, h, slot + 16) : -1;
+        uint32_t there = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u;
+        if (lo < 0) there &= 0xffff0000u;
+        if (hi < 0) there &= 0x0000ffffu;
+        mine[n] = bits_of_group(there, g);
+        KeyLoads<S> raw;
+        raw.request(a.c.k, lo, hi, lane);
+        if constexpr (DT == BRL_I8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) kf[n][e] = a.c.ks[((e < 4 ? lo : hi) < 0 ? 0 : (e < 4 ? lo : hi)) + 4 * g + (e & 3)];
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int s = 0; s < S::KS; ++s) raw.fragment(t, s, lane, key[n][t][s]);
     }
-    v8h key[2][S::KS][S::PL];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int s = 0; s < S::KS; ++s) raw.fragment(t, s, lane, key[t][s]);
-    const uint32_t mine = bits_of_group(there, g);
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const int token0 = a.tree || slot0 <= st.base ? 0 : slot0 - st.base;          // the first token that sees the block's first slot
-    for (int rt = token0 * p.group.n / 16; rt * 16 < rows; ++rt) {
-        const uint4* q = p.q + (((size_t)unit * p.rows_pad / 16 + rt) * S::KS * 2) * 64 + lane;
-        const int r = rt * 16 + c;
-        const float lse = r < rows ? p.lse[(size_t)unit * p.rows_pad + r] : INFINITY;
-        v4f acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    float sum[NB][8] = {};
+    const int token0 = a.tree || slot0 <= st.base ? 0 : slot0 - st.base;          // the first token that sees the first slot
+    const int tiles = (rows + 15) / 16;
+    int rt = token0 * p.group.n / 16 + part;
+    v8h qh[2][S::KS], ql[2][S::KS];                                    // of the tile worked on and of the next
+    float lse[2];
+    auto request = [&](int t, int i) __attribute__((always_inline)) {
+        if (t >= tiles) t = tiles - 1;                                 // (not used)
+        const uint4* q = p.q + (((size_t)unit * p.rows_pad / 16 + t) * S::KS * 2) * 64 + lane;
 #pragma unroll
         for (int s = 0; s < S::KS; ++s) {
-            const v8h qh = __builtin_bit_cast(v8h, q[s * 128]), ql = __builtin_bit_cast(v8h, q[s * 128 + 64]);
+            qh[i][s] = __builtin_bit_cast(v8h, q[s * 128]);
+            ql[i][s] = __builtin_bit_cast(v8h, q[s * 128 + 64]);
+        }
+        const int r = t * 16 + c;
+        lse[i] = p.lse[(size_t)unit * p.rows_pad + (r < rows ? r : rows - 1)];
+    };
+    auto add = [&](int t, int i) __attribute__((always_inline)) {
+        const int r = t * 16 + c, token = p.group.token(r < rows ? r : rows - 1);
+        const int all_see = st.base + (a.tree ? 0 : p.group.token(t * 16) + 1);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if constexpr (S::PL == 2) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[t][s][1], qh, acc[t], 0, 0, 0);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[t][s][0], ql, acc[t], 0, 0, 0);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[t][s][0], qh, acc[t], 0, 0, 0);
+        for (int n = 0; n < NB; ++n) {
+            v4f acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+            for (int s = 0; s < S::KS; ++s) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if constexpr (S::PL == 2) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[n][t][s][1], qh[i][s], acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[n][t][s][0], ql[i][s], acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[n][t][s][0], qh[i][s], acc[t], 0, 0, 0);
+                }
+            }
+            uint32_t bits = r < rows ? mine[n] : 0u;
+            if (slot0 + 32 * n + 32 > all_see) bits &= bits_of_group(visible_bits(a, st, token, slot0 + 32 * n), g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float x = acc[e >> 2][e & 3];
+                if constexpr (DT == BRL_I8) x *= kf[n][e];
+                sum[n][e] += bits >> e & 1u ? __builtin_amdgcn_exp2f(x - lse[i]) : 0.f;
             }
         }
-        const int token = p.group.token(r < rows ? r : rows - 1);
-        uint32_t bits = mine;
-        if (slot0 + 32 > st.base + (a.tree ? 0 : p.group.token(rt * 16) + 1)) bits &= bits_of_group(visible_bits(a, st, token, slot0), g);
+    };
+    request(rt, 0);
+    for (; rt < tiles; rt += 2 * p.w_parts) {
+        request(rt + p.w_parts, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        add(rt, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (rt + p.w_parts >= tiles) break;
+        request(rt + 2 * p.w_parts, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        add(rt + p.w_parts, 1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    float* y = p.w_parts == 1 ? a.weights + (size_t)unit * a.ld_weights + slot0 : p.part_w + ((size_t)part * units + unit) * p.ld_scores + slot0;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float x = acc[e >> 2][e & 3];
-            if constexpr (DT == BRL_I8) x *= kf[e];
-            sum[e] += bits >> e & 1u ? __builtin_amdgcn_exp2f(x - lse) : 0.f;
+            float x = sum[n][e];
+            x += lane_exchange<DPP_XOR1>(x);
+            x += lane_exchange<DPP_XOR2>(x);
+            x += lane_exchange<DPP_HALF_MIRROR>(x);
+            x += lane_exchange<DPP_MIRROR>(x);
+            if (c != 0) continue;
+            if (p.w_parts > 1) y[32 * n + key_of_score(g, e)] = x;
+            else if (mine[n] >> e & 1u) y[32 * n + key_of_score(g, e)] += x;
         }
     }
-    float* y = a.weights + (size_t)unit * a.ld_weights + slot0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float x = sum[e];
-        x += lane_exchange<DPP_XOR1>(x);
-        x += lane_exchange<DPP_XOR2>(x);
-        x += lane_exchange<DPP_HALF_MIRROR>(x);
-        x += lane_exchange<DPP_MIRROR>(x);
-        if (c == 0 && mine >> e & 1u) y[key_of_score(g, e)] += x;
-    }
+}
+// the parts of the rows added up, in their order: a thread per slot
+__global__ __launch_bounds__(256) void cached_sum_weights_kernel(CachedAttention a, Plan p, int chunks) {
+    const int unit = blockIdx.x / chunks, slot = blockIdx.x % chunks * 256 + threadIdx.x;
+    const StateTokens st = state_tokens(a.t, a.c, unit / a.c.n_kv);
+    if (st.n == 0 || slot >= st.len) return;
+    const float* x = p.part_w + (size_t)unit * p.ld_scores + slot;
+    float w = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < p.w_parts; ++i) w += x[(size_t)i * a.t.B * a.c.n_kv * p.ld_scores];
+    a.weights[(size_t)unit * a.ld_weights + slot] += w;
 }
 
 struct Layout {
     Plan p;
     bool tiles;               // many rows
     int waves, rt;            // few rows: wavefronts of a workgroup; many: row tiles of a wavefront
-    size_t o_off, ml_off, lse_off, scores_off, q_off, total;
+    size_t o_off, ml_off, lse_off, scores_off, q_off, w_off, total;
 };
 
 Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int max_len, bool weights) {
@@ -1431,6 +1488,15 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
         L.lse_off = take(rows * 4);
         if (L.tiles) {
             L.q_off = take(rows * ((c.dh + 31) / 32) * 32 * 4);
+            // A block's wavefront walks the row tiles one after the other: parts until there are four wavefronts per SIMD, of four tiles at
+            // least.  us of a call, one part / so: 2 heads of 16, 1800 slots, 950 x 4 rows 239 / 42; 10 of 128, 2800 slots, int8, 5900
+            // rows 1076 / 328; 5 of 128, 512 slots, fp32, 2048 rows 190 / 52.
+            const int own = c.dtype == BRL_F32 ? WeightBlocks<BRL_F32>::N : WeightBlocks<BRL_F16>::N, row_blocks = (blocks + own - 1) / own;
+            const long long want = 4096 / ((long long)units * row_blocks), most = (p.rows_max + 63) / 64;
+            p.w_parts = want > most ? (int)most : want > 1 ? (int)want : 1;
+            if (p.w_parts > 32) p.w_parts = 32;
+            p.ld_scores = (size_t)row_blocks * own * 32;
+            if (p.w_parts > 1) L.w_off = take((size_t)p.w_parts * units * p.ld_scores * 4);
         } else {
             p.ld_scores = (size_t)blocks * 32;
             L.scores_off = take((size_t)units * p.rows_max * p.ld_scores * 4);
@@ -1475,9 +1541,15 @@ int launch_many(const CachedAttention& a, const Layout& L, hipStream_t s) {
         BRL_LAUNCH_CHECK("cached_join_splits_kernel");
     }
     if (a.weights) {
-        const int chunks = (a.t.max_len + 127) / 128;
-        hipLaunchKernelGGL((cached_tile_weights_kernel<DT, DH>), dim3((unsigned)(units * chunks)), block, 0, s, a, p, chunks);
+        constexpr int SLOTS = 128 * WeightBlocks<DT>::N;               // of a workgroup
+        const int chunks = (a.t.max_len + SLOTS - 1) / SLOTS;
+        hipLaunchKernelGGL((cached_tile_weights_kernel<DT, DH>), dim3((unsigned)(units * chunks * p.w_parts)), block, 0, s, a, p, chunks);
         BRL_LAUNCH_CHECK("cached_tile_weights_kernel");
+        if (p.w_parts > 1) {
+            const int all = (a.t.max_len + 255) / 256;
+            hipLaunchKernelGGL(cached_sum_weights_kernel, dim3((unsigned)(units * all)), dim3(256), 0, s, a, p, all);
+            BRL_LAUNCH_CHECK("cached_sum_weights_kernel");
+        }
     }
     return BRL_OK;
 }
@@ -1507,8 +1579,10 @@ int launch_cached_attention(const CachedAttention& a, void* workspace, hipStream
     p.part_ml = reinterpret_cast<float2*>(base + L.ml_off);
     if (a.weights) {
         p.lse = reinterpret_cast<float*>(base + L.lse_off);
-        if (L.tiles) p.q = reinterpret_cast<uint4*>(base + L.q_off);
-        else p.scores = reinterpret_cast<float*>(base + L.scores_off);
+        if (L.tiles) {
+            p.q = reinterpret_cast<uint4*>(base + L.q_off);
+            p.part_w = reinterpret_cast<float*>(base + L.w_off);
+        } else p.scores = reinterpret_cast<float*>(base + L.scores_off);
     }
     LaunchTimer tm(BRL_KC_ATTENTION, s);
     return a.c.dtype == BRL_F32 ? launch_typed<BRL_F32>(a, L, s) : a.c.dtype == BRL_F16 ? launch_typed<BRL_F16>(a, L, s)
