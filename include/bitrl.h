@@ -406,6 +406,8 @@ int attention_forward(const float* qkv, int B, int S,
  *   weights, DEVICE [B, n_kv_heads, ld_weights] or NULL: weights[b, h, j] += sum
  *   over the state's new tokens and the query heads of k/v head h of the softmax
  *   weight of slot j, in a fixed order.
+ *   The workspace query answers for the arguments that it is given; a call with
+ *   smaller bounds can need more (work is split otherwise).
  *
  * attention_cache_select: which slots to keep.  Where lens[b] > keep: the first
  *   `first`, the last `recent`, and between them the keep - first - recent with
