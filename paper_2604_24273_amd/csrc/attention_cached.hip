@@ -1465,7 +1465,7 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
         L.rt = p.rows_max <= 64 ? 1 : 2;
         p.row_blocks = (p.rows_max + 64 * L.rt - 1) / (64 * L.rt);
         p.rows_pad = p.row_blocks * 64 * L.rt;
-        // 512 workgroups run at a time.
+        // (512 workgroups run at a time.)
         const long long groups = (long long)units * p.row_blocks;
         const int new_blocks = (max_new + 31) / 32, most = blocks / 8 < 64 ? blocks / 8 : 64;
         if (4 * new_blocks < blocks) {
@@ -1479,8 +1479,8 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
         } else {
             // Mostly new tokens: workgroups of every length, the longest first, fill the rounds by themselves, and there are many rows
             // to be joined: only until all units have work.  1 / 2 / 3 / 4 parts, us: 650 workgroups (2 x 2000 tokens, 5 groups of 4 heads of
-            // 128, fp16) 115 / 144 / 171 / 184; 640 205 / 225 / 250 / 251; 512 (heads of 100) 105 / 128 / 139 / 152; 256 (fp32) 80 / 68 / 80 / 85; 235 (fp32)
-            // 107 / 84 / 81 / 90; 136 (heads of 64) 64 / 46 / 39 / 37.
+            // 128, fp16) 115 / 144 / 171 / 184; 640 205 / 225 / 250 / 251; 512 (heads of 100) 105 / 128 / 139 / 152; 256 (fp32) 80 / 68 /
+            // 80 / 85; 235 (fp32) 107 / 84 / 81 / 90; 136 (heads of 64) 64 / 46 / 39 / 37.
             const long long s = 640 / groups;
             p.splits = s < 1 || most < 1 ? 1 : s < most ? (int)s : most;
         }
@@ -1502,7 +1502,8 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
             // A block's wavefront walks the row tiles one after the other: parts until there are four wavefronts per SIMD, of four tiles at
             // least.  us of a call, one part / so: 2 heads of 16, 1800 slots, 7600 rows 239 / 42; 10 of 128, 2800 slots, int8, 5900
             // rows 1076 / 328; 5 of 128, 512 slots, fp32, 2048 rows 190 / 52.
-            const int own = c.dtype == BRL_F32 ? WeightBlocks<BRL_F32>::N : WeightBlocks<BRL_F16>::N, row_blocks = (blocks + own - 1) / own;
+            const int own = c.dtype == BRL_F32 ? WeightBlocks<BRL_F32>::N : WeightBlocks<BRL_F16>::N;
+            const int row_blocks = (blocks + own - 1) / own;             // wavefronts that it takes for a unit's keys
             const long long want = 4096 / ((long long)units * row_blocks), most = (p.rows_max + 63) / 64;
             p.w_parts = want > most ? (int)most : want > 1 ? (int)want : 1;
             if (p.w_parts > 32) p.w_parts = 32;

@@ -919,3 +919,105 @@ def test_select_from_rows_on_any_four_bytes(ld, shift):
     B.attention_cache_select(t, 2, 3, R.dev(lens), 3000, 500, 3, 50, kept, counts)
     want, n = K.select(w, lens, 500, 3, 50)
     assert np.array_equal(kept.cpu().numpy(), want) and np.array_equal(counts.cpu().numpy(), n)
+
+
+# ---------------------------------------------------------------- the same call again
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "i8"])
+@pytest.mark.parametrize("dh,hq,hkv,page,cached,new", [
+    (128, 8, 2, 64, [10, 300], [130, 77]),                        # shared blocks, weights in parts
+    (64, 4, 2, 32, [1500, 3], [1, 2]),                            # the shared list
+    (32, 6, 2, 16, [100, 40], [2, 1]),                            # a workgroup each
+])
+def test_captured_calls_with_weights_repeat_themselves(dh, hq, hkv, page, cached, new, dtype):
+    """append, attention with weights, selection and moving in one graph: every replay gives the eager calls' bits.  In between the program
+    works and synchronizes, and the cache, weights and workspace are put back or spoiled."""
+    B, R = _mods()
+    lens = [a + n for a, n in zip(cached, new)]
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T, keep = int(cu[-1]), max(lens) // 2
+    cos, sin = tables(max(lens), dh)
+    c = make_cache(71, hkv, dh, page, lens, DTYPES[dtype])
+    g = OnGpu(B, R, c, dh, cos, sin)
+    start = {n: x.clone() for n, x in g.t.items()}
+    qkv = R.dev(synth.normal(71, dh, (T, (hq + 2 * hkv) * dh)))
+    cu_d, lens_d = g.ints(cu), g.ints(lens)
+    w0 = torch.rand(len(lens), hkv, max(lens), device="cuda")
+    w, out = w0.clone(), torch.empty(T, hq * dh, device="cuda")
+    kept = torch.empty(len(lens), hkv, keep, dtype=torch.int32, device="cuda")
+    counts = torch.empty(len(lens), dtype=torch.int32, device="cuda")
+    ws = torch.empty(B.brl_attention_cached_workspace_bytes(g.struct, hq, T, len(lens), max(new), max(lens), True), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        B.attention_cache_append(g.struct, qkv, hq, T, len(lens), cu_d, max(new), lens_d, None, g.cos, g.sin)
+        B.attention_cached_forward(g.struct, qkv, hq, T, len(lens), cu_d, max(new), lens_d, max(lens), None, g.cos, g.sin, None, out, w, ws)
+        B.attention_cache_select(w, len(lens), hkv, lens_d, max(lens), keep, 2, keep // 4, kept, counts)
+        B.attention_cache_compact(g.struct, len(lens), lens_d, max(lens), kept, hkv, None, counts, w)
+
+    def reset():
+        for n, x in g.t.items():
+            x.copy_(start[n])
+        w.copy_(w0)
+        ws.fill_(255)
+        out.fill_(float("nan"))
+        kept.fill_(-7)
+        counts.fill_(-7)
+
+    def state():
+        torch.cuda.synchronize()
+        return [x.cpu().numpy().copy() for x in (out, w, kept, counts, *g.t.values())]
+
+    reset()
+    calls()
+    eager = state()
+    reset()
+    calls()
+    assert all(same_bits(a, b) for a, b in zip(eager, state()))
+    reset()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(4):
+        reset()
+        graph.replay()
+        got = state()
+        assert all(same_bits(a, b) for a, b in zip(eager, got))
+        torch.randn(1000, 1000, device="cuda").sum().item()
+
+
+def test_two_streams_at_once():
+    """Two calls in flight on two streams, each with its own cache, workspace and outputs, give what each gives alone."""
+    B, R = _mods()
+    dh, hq, hkv, page = 64, 4, 2, 32
+    cos, sin = tables(3000, dh)
+    jobs = []
+    for i, (cached, new) in enumerate((([2500, 900], [2, 1]), ([400, 30], [90, 60]))):
+        lens = [a + n for a, n in zip(cached, new)]
+        cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        g = OnGpu(B, R, make_cache(81 + i, hkv, dh, page, lens, np.float16), dh, cos, sin)
+        T = int(cu[-1])
+        j = dict(g=g, T=T, new=max(new), longest=max(lens), qkv=R.dev(synth.normal(81, i, (T, (hq + 2 * hkv) * dh))), cu=g.ints(cu), lens=g.ints(lens),
+                 stream=torch.cuda.Stream())
+        j["ws"] = torch.empty(B.brl_attention_cached_workspace_bytes(g.struct, hq, T, 2, j["new"], j["longest"], True), dtype=torch.uint8, device="cuda")
+        jobs.append(j)
+
+    def run(j, out, w):
+        B.attention_cached_forward(j["g"].struct, j["qkv"], hq, j["T"], 2, j["cu"], j["new"], j["lens"], j["longest"], None, j["g"].cos, j["g"].sin,
+                                   None, out, w, j["ws"])
+
+    def outputs(n):
+        return [[(torch.empty(j["T"], hq * dh, device="cuda"), torch.zeros(2, hkv, j["longest"], device="cuda")) for _ in range(n)] for j in jobs]
+
+    alone, together = outputs(1), outputs(20)
+    for j, o in zip(jobs, alone):
+        run(j, *o[0])
+    torch.cuda.synchronize()
+    for i in range(20):
+        for j, o in zip(jobs, together):
+            with torch.cuda.stream(j["stream"]):
+                run(j, *o[i])
+    torch.cuda.synchronize()
+    for a, many in zip(alone, together):
+        for o in many:
+            assert torch.equal(o[0], a[0][0]) and torch.equal(o[1], a[0][1])
