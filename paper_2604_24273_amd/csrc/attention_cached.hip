@@ -1480,8 +1480,9 @@ Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int 
             // Mostly new tokens: workgroups of every length, the longest first, fill the rounds by themselves, and there are many rows
             // to be joined: only until all units have work.  1 / 2 / 3 / 4 parts, us: 650 workgroups (2 x 2000 tokens, 5 groups of 4 heads of
             // 128, fp16) 115 / 144 / 171 / 184; 640 205 / 225 / 250 / 251; 512 (heads of 100) 105 / 128 / 139 / 152; 256 (fp32) 80 / 68 /
-            // 80 / 85; 235 (fp32) 107 / 84 / 81 / 90; 136 (heads of 64) 64 / 46 / 39 / 37.
-            const long long s = 640 / groups;
+            // 80 / 85; 235 (fp32) 107 / 84 / 81 / 90; 136 (heads of 64) 64 / 46 / 39 / 37.  160 (1 x 1000, fp16): 44 with 3, 54 with 4; 188 (heads
+            // of 16): 39 with 2, 32 with 3.
+            const long long s = 576 / groups;
             p.splits = s < 1 || most < 1 ? 1 : s < most ? (int)s : most;
         }
         parts = p.splits > 1 ? (size_t)units * p.rows_pad * p.splits : 0;
@@ -1548,7 +1549,9 @@ int launch_many(const CachedAttention& a, const Layout& L, hipStream_t s) {
     if (p.splits > 1) {
         constexpr int PER = Joiner<DH, 1>::PER;
         const unsigned rows = (unsigned)(units * p.rows_max);
-        if (p.splits <= 4) hipLaunchKernelGGL((cached_join_splits_kernel<DH, PER>), dim3((rows + PER - 1) / PER), dim3(256), 0, s, a, p);
+        // (a workgroup for several rows where the parts are few or the rows many: 1 x 2000 tokens, 8 heads of 32, 5 parts: 24 us a call, 33 with
+        // one for each)
+        if (p.splits <= 4 || rows > 4096) hipLaunchKernelGGL((cached_join_splits_kernel<DH, PER>), dim3((rows + PER - 1) / PER), dim3(256), 0, s, a, p);
         else hipLaunchKernelGGL((cached_join_splits_kernel<DH, 1>), dim3(rows), dim3(256), 0, s, a, p);
         BRL_LAUNCH_CHECK("cached_join_splits_kernel");
     }
