@@ -235,7 +235,7 @@ class KVCache:
 
     def append(self, qkv: torch.Tensor, new: Sequence[int], depths: Optional[Sequence[int]] = None) -> None:
         """Stores the keys and values of new[b] tokens per state.  depths: per token its distance behind the state's tokens (of a
-        tree of candidates), None for one after the other."""
+        tree of candidates), None for one after the other.  A call that is refused leaves everything as it was."""
         new = np.asarray(new, dtype=np.int32)
         width = (self.n_heads + 2 * self.n_kv_heads) * self.head_dim
         if new.shape != (self.states,) or (new < 0).any() or int(new.sum()) < 1:
@@ -254,10 +254,15 @@ class KVCache:
             raise ValueError("a token's position is behind the rotary tables' %d" % self.rope_cos.shape[0])
         qkv = qkv.contiguous()
         began = (self.lens_host.copy(), self.seen.copy())
+        last = (qkv, new, total, dev(cu), dev(pos.astype(np.int32)), began)
         self._resize(self.lens_host + new)
-        self._last = (qkv, new, total, dev(cu), dev(pos.astype(np.int32)), began)
-        B.attention_cache_append(self.struct, qkv, self.n_heads, total, self.states, self._last[3], int(new.max()), self.lens,
-                                 self._last[4], self.rope_cos, self.rope_sin)
+        try:
+            B.attention_cache_append(self.struct, qkv, self.n_heads, total, self.states, last[3], int(new.max()), self.lens, last[4],
+                                     self.rope_cos, self.rope_sin)
+        except BaseException:
+            self._resize(began[0])                              # slots that nothing was stored in are nobody's
+            raise
+        self._last = last
         for b in range(self.states):
             if new[b]:
                 self.seen[b] = int(pos[cu[b]:cu[b + 1]].max()) + 1
