@@ -214,6 +214,7 @@ class KVCache:
         self.weights = torch.zeros((states, n_kv_heads, max_tokens), device=DEV) if track_weights else None
         self.ws: Optional[Workspace] = None
         self._last = None                                       # the last append: rows, tokens, positions, where they began
+        self._counted = False                                   # whether its attention is in the weights
 
     def _resize(self, lens: np.ndarray) -> None:
         """States have `lens` slots from here on: pages are given out or freed; lengths and pages go to the device."""
@@ -262,27 +263,30 @@ class KVCache:
         except BaseException:
             self._resize(began[0])                              # slots that nothing was stored in are nobody's
             raise
-        self._last = last
+        self._last, self._counted = last, False
         for b in range(self.states):
             if new[b]:
                 self.seen[b] = int(pos[cu[b]:cu[b + 1]].max()) + 1
 
     def attend(self, tree_mask: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention [tokens, n_heads * head_dim] of the last append's tokens over everything that their states hold.
-        tree_mask: int32 [tokens, words], bit j of a token's row: it sees its state's new token j."""
+        tree_mask: int32 [tokens, words], bit j of a token's row: it sees its state's new token j.  The first call after an append
+        adds to the tracked weights, further ones do not.  The queries are read from append's qkv, which has to stay as it was."""
         if self._last is None:
             raise ValueError("attend follows append")
         qkv, new, total, cu, pos, _ = self._last
         if tree_mask is not None and (tree_mask.dtype != torch.int32 or tree_mask.dim() != 2 or tree_mask.shape[0] != total):
             raise ValueError("tree_mask must be int32 [%d, words]" % total)
         longest, max_len = int(new.max()), int(self.lens_host.max())
+        weights = None if self._counted else self.weights
         need = B.brl_attention_cached_workspace_bytes(self.struct, self.n_heads, total, self.states, longest, max_len,
-                                                      self.weights is not None)
+                                                      weights is not None)
         self.ws = Workspace(need) if self.ws is None else self.ws.ensure(need)
         out = torch.empty((total, self.n_heads * self.head_dim), dtype=torch.float32, device=DEV)
         B.attention_cached_forward(self.struct, qkv, self.n_heads, total, self.states, cu, longest, self.lens, max_len, pos,
                                    self.rope_cos, self.rope_sin, None if tree_mask is None else tree_mask.contiguous(), out,
-                                   self.weights, self.ws.buf)
+                                   weights, self.ws.buf)
+        self._counted = True
         return out
 
     def _settle(self, lens: np.ndarray) -> None:

@@ -74,3 +74,23 @@ def test_a_refused_append_changes_nothing(holder):
     kv.append(rows(21), [18, 3])                                          # the same once more
     assert kv.lens_host.tolist() == [38, 6] and kv.seen.tolist() == [38, 6] and kv.lens.tolist() == [38, 6]
     assert [len(p) for p in kv.pages] == [3, 1] and len(kv.free) == 8 - 4
+
+
+def test_the_attention_of_an_append_is_added_up_once(holder):
+    """Attending again (another mask, a call that was refused) gives outputs, but no slot its weight a second time."""
+    make, fake = holder
+    kv = make(track_weights=True)
+    for new in ([5, 2], [1, 0]):
+        kv.append(rows(sum(new)), new)
+        fake.refuse = "attention_cached_forward"
+        with pytest.raises(ValueError, match="refused"):
+            kv.attend()
+        begin = len(fake.named("attention_cached_forward"))
+        kv.attend()
+        kv.attend(torch.ones(sum(new), 1, dtype=torch.int32))
+        fake.refuse = "attention_cache_append"
+        with pytest.raises(ValueError, match="refused"):
+            kv.append(rows(1), [1, 0])
+        kv.attend()
+        calls = fake.named("attention_cached_forward")[begin:]
+        assert [c[13] is not None for c in calls] == [True, False, False]
