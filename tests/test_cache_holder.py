@@ -93,4 +93,4 @@ def test_the_attention_of_an_append_is_added_up_once(holder):
             kv.append(rows(1), [1, 0])
         kv.attend()
         calls = fake.named("attention_cached_forward")[begin:]
-        assert [c[13] is not None for c in calls] == [True, False, False]
+        assert [c[14] is not None for c in calls] == [True, False, False]
