@@ -208,7 +208,7 @@ class KVCache:
         self.rope_cos, self.rope_sin = (torch.empty((n, head_dim // 2), device=DEV) for _ in range(2))
         B.attention_rope_table(self.rope_cos, self.rope_sin, head_dim, rope_theta)
         self.lens_host = np.zeros(states, dtype=np.int32)       # slots in use
-        self.seen = np.zeros(states, dtype=np.int32)            # tokens that a state has had: its next position
+        self.seen = np.zeros(states, dtype=np.int32)            # a state's next position
         self.pages: List[List[int]] = [[] for _ in range(states)]
         self.free = list(range(n_pages - 1, -1, -1))
         self.weights = torch.zeros((states, n_kv_heads, max_tokens), device=DEV) if track_weights else None
@@ -254,7 +254,7 @@ class KVCache:
         if pos.max() >= self.rope_cos.shape[0]:
             raise ValueError("a token's position is behind the rotary tables' %d" % self.rope_cos.shape[0])
         qkv = qkv.contiguous()
-        began = (self.lens_host.copy(), self.seen.copy())
+        began = (self.lens_host.copy(), self.seen.copy(), pos)
         last = (qkv, new, total, dev(cu), dev(pos.astype(np.int32)), began)
         self._resize(self.lens_host + new)
         try:
@@ -313,10 +313,10 @@ class KVCache:
 
     def keep_branch(self, branches: Sequence[Sequence[int]]) -> None:
         """Of the last append's tokens of each state those whose indices (ascending) are given stay, one behind the other, and
-        the state goes on behind them; the rest is dropped."""
+        the state goes on behind the farthest position among them; the rest is dropped."""
         if self._last is None:
             raise ValueError("keep_branch follows append")
-        new, (start, seen) = self._last[1], self._last[5]
+        new, (start, seen, pos) = self._last[1], self._last[5]
         if len(branches) != self.states or any(list(x) != sorted(set(x)) or (len(x) and not 0 <= x[0] <= x[-1] < n)
                                                for x, n in zip(branches, new)):
             raise ValueError("a branch is ascending indices of the state's last tokens, one list per state")
@@ -327,7 +327,8 @@ class KVCache:
         B.attention_cache_compact(self.struct, self.states, self.lens, self.max_tokens, dev(kept), 1, dev(start), dev(counts),
                                   self.weights)
         self._settle(start + counts)
-        self.seen = seen + counts
+        first = np.cumsum(new) - new
+        self.seen = np.array([max([n] + [int(pos[r + i]) + 1 for i in x]) for n, r, x in zip(seen, first, branches)], dtype=np.int32)
 
 
 class HeadHandle:

@@ -94,3 +94,19 @@ def test_the_attention_of_an_append_is_added_up_once(holder):
         kv.attend()
         calls = fake.named("attention_cached_forward")[begin:]
         assert [c[14] is not None for c in calls] == [True, False, False]
+
+
+def test_a_state_goes_on_behind_the_tokens_that_it_keeps(holder):
+    """The next token's position is behind the last one kept, also where the kept ones are no whole path from the first."""
+    make, fake = holder
+    kv = make(states=4)
+    position = lambda: fake.named("attention_cache_append")[-1][8].tolist()  # noqa: E731
+    kv.append(rows(8), [2, 2, 2, 2])
+    kv.append(rows(11), [3, 4, 4, 0], [0, 1, 2, 0, 0, 1, 2, 0, 1, 2, 3])
+    kv.keep_branch([[0, 2], [1, 2, 3], [], []])                           # its middle dropped; a path; nothing; nothing new
+    assert kv.lens_host.tolist() == [4, 5, 2, 2]
+    kv.append(rows(5), [2, 1, 1, 1])
+    assert position() == [5, 6, 5, 2, 2]
+    kv.keep_branch([[1], [0], [0], []])
+    kv.append(rows(4), [1, 1, 1, 1])
+    assert position() == [7, 6, 3, 2]
