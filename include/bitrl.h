@@ -389,6 +389,8 @@ int attention_forward(const float* qkv, int B, int S,
  * attention_cache_append: rotates the new keys, stores keys and values.
  *   fp16: rounded to nearest (|x| < 65504).  int8, per row: a = max(max|x|,
  *   1e-30), code = clamp(rne(x * (127 / a)), -127, 127), scale = a / 127.
+ *   A row with an infinite or NaN component is codes of zero under an infinite
+ *   or NaN scale: all of it is no number.
  *
  * attention_cached_forward: out [T, n_heads * head_dim] fp32 = softmax(q k^T /
  *   sqrt(head_dim)) v over the slots that the token sees; query head h reads k/v

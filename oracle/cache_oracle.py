@@ -39,8 +39,10 @@ def rotate(x, cos, sin):
 
 
 def quantise_row(x):
-    """int8 codes and fp32 scale of one row."""
+    """int8 codes and fp32 scale of one row; zeros under a scale that is infinite or NaN where a component is."""
     a = np.maximum(np.abs(x).max(), SMALLEST).astype(F32)
+    if not np.isfinite(a):
+        return np.zeros(x.shape, dtype=np.int8), F32(a / F32(127))
     codes = np.clip(np.rint((x * (F32(127) / a)).astype(F32)), -127, 127).astype(np.int8)
     return codes, F32(a / F32(127))
 

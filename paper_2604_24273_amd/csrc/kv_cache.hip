@@ -59,21 +59,34 @@ __device__ __forceinline__ void store_elements(char* row, int d, const Floats<VW
 }
 
 template <int DT, int VW, int GS>
-__device__ __forceinline__ void store_row(char* pool, float* scales, int idx, int rowlen, int dh, const Floats<VW>& a,
-                                          const Floats<VW>& b, int lane) {
+__device__ __forceinline__ void store_row(char* pool, float* scales, int idx, int rowlen, int dh, Floats<VW> a, Floats<VW> b, int lane) {
     const int half = dh / 2;
     const bool mine = lane * VW < half;
     float s = 0.f;
     if constexpr (DT == BRL_I8) {
-        float m = 0.f;
+        // |x| in the order of its bits: a NaN is above infinity and so becomes the row's scale
+        uint32_t top = 0;
 #pragma unroll
-        for (int e = 0; e < VW; ++e) m = fmaxf(m, fmaxf(fabsf(a.x[e]), fabsf(b.x[e])));
-        if (!mine) m = 0.f;
+        for (int e = 0; e < VW; ++e) {
+            const uint32_t x = __float_as_uint(a.x[e]) & 0x7fffffffu, y = __float_as_uint(b.x[e]) & 0x7fffffffu;
+            top = top > x ? top : x;
+            top = top > y ? top : y;
+        }
+        if (!mine) top = 0;
 #pragma unroll
-        for (int x = 1; x < GS; x <<= 1) m = fmaxf(m, __shfl_xor(m, x, 64));
-        m = fmaxf(m, 1e-30f);
+        for (int x = 1; x < GS; x <<= 1) {
+            const uint32_t y = __shfl_xor(top, x, 64);
+            top = top > y ? top : y;
+        }
+        float m = __uint_as_float(top);
+        m = m < 1e-30f ? 1e-30f : m;
         s = 127.f / m;
         if (lane == 0) scales[idx] = m / 127.f;
+        if (!(m < INFINITY)) {                                    // no numbers in this row: codes of zero
+#pragma unroll
+            for (int e = 0; e < VW; ++e) a.x[e] = b.x[e] = 0.f;
+            s = 0.f;
+        }
     }
     char* row = pool + (size_t)idx * rowlen * kv_bytes(DT);
     if (mine) {
