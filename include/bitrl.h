@@ -403,7 +403,8 @@ int attention_forward(const float* qkv, int B, int S,
  *   A token that sees nothing gives zeros.  Queries and the cache's values within
  *   |x| < 65504 (on the matrix cores queries and BRL_F32 rows are fp16 hi + lo
  *   pairs, as in BRL_ATTN_MFMA: a number is carried to 2^-22 of itself or to 3e-8,
- *   whichever is more).  What is infinite or NaN in a slot reaches the tokens that see
+ *   whichever is more; a probability to 2^-22 of itself or to 2^-37 of the largest
+ *   that the query row has).  What is infinite or NaN in a slot reaches the tokens that see
  *   the slot and no others.
  *   weights, DEVICE [B, n_kv_heads, ld_weights] or NULL: weights[b, h, j] += sum
  *   over the state's new tokens and the query heads of k/v head h of the softmax

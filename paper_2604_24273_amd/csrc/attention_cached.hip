@@ -26,9 +26,10 @@ typedef __fp16 v4fp __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.4426950408889634f;
-// Probabilities are carried as 2^(s - m + P_SHIFT) with m the running maximum, which follows the true one only once that is
-// P_SLACK ahead: at most 2^14, inside fp16, while parts down to 2^-38 of the largest keep their hi and lo planes apart.
-constexpr float P_SHIFT = 6.f, P_SLACK = 8.f;
+// Probabilities are carried as 2^(s - m + P_SHIFT), m the running maximum rounded up to a whole number (so that going over to another one
+// multiplies by powers of two), which follows the true one only once that is P_SLACK ahead: at most 2^15, inside fp16.  The smallest
+// step of the lo plane is 2^-24, so each is carried to 2^-22 of itself or to 2^-37 of the row's largest, which is 2^12 or more.
+constexpr float P_SHIFT = 13.f, P_SLACK = 2.f;
 
 // fp16 hi and lo of two values, each rounded once (x - hi is exact; the multiply-add rounds it to fp16 directly)
 __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t& hi, uint32_t& lo) {
@@ -431,7 +432,7 @@ struct RowState {
         if (__any(top > m + P_SLACK)) {
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float m_new = fmaxf(m, top), ref_new = m_new == -INFINITY ? 0.f : m_new - P_SHIFT;
+            const float m_new = fmaxf(m, ceilf(top)), ref_new = m_new == -INFINITY ? 0.f : m_new - P_SHIFT;
             const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - ref_new);
             l *= alpha;
             scale(alpha);
