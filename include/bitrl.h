@@ -401,11 +401,14 @@ int attention_forward(const float* qkv, int B, int S,
  *   set (a set bit for itself and for its ancestors: candidate texts as branches of one
  *   prefix, evaluated together); tokens from 32 * mask_words on are not seen.
  *   A token that sees nothing gives zeros.  Queries and the cache's values within
- *   |x| < 65504 (on the matrix cores queries and BRL_F32 rows are fp16 hi + lo
+ *   |x| < 65504.  On the matrix cores queries and BRL_F32 rows are fp16 hi + lo
  *   pairs, as in BRL_ATTN_MFMA: a number is carried to 2^-22 of itself or to 3e-8,
- *   whichever is more; a probability to 2^-22 of itself or to 2^-37 of the largest
- *   that the query row has).  What is infinite or NaN in a slot reaches the tokens that see
- *   the slot and no others.
+ *   whichever is more.  A probability is carried to 2^-22 of itself or to 2^-37 of
+ *   the largest that its query row has; with BRL_I8 its product with the slot's
+ *   value scale, to 2^-35 of the largest such product or (values below 1e-25) to
+ *   1e-31 in the output.  Slots that a token does not see have no part in this.
+ *   What is infinite or NaN in a slot reaches the tokens that see the slot and no
+ *   others.
  *   weights, DEVICE [B, n_kv_heads, ld_weights] or NULL: weights[b, h, j] += sum
  *   over the state's new tokens and the query heads of k/v head h of the softmax
  *   weight of slot j, in a fixed order.

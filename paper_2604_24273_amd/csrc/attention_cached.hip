@@ -26,10 +26,15 @@ typedef __fp16 v4fp __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.4426950408889634f;
-// Probabilities are carried as 2^(s - m + P_SHIFT), m the running maximum rounded up to a whole number (so that going over to another one
-// multiplies by powers of two), which follows the true one only once that is P_SLACK ahead: at most 2^15, inside fp16.  The smallest
-// step of the lo plane is 2^-24, so each is carried to 2^-22 of itself or to 2^-37 of the row's largest, which is 2^12 or more.
-constexpr float P_SHIFT = 13.f, P_SLACK = 2.f;
+// Probabilities are carried as 2^(s - m + SHIFT), m the running maximum rounded up to a whole number (so that going over to another one
+// multiplies by powers of two), which follows the true one only once that is SLACK ahead: at most 2^15, inside fp16.  The smallest step of
+// the lo plane is 2^-24, so each is carried to 2^-22 of itself or to 2^(-24 - SHIFT) of the row's largest, which is 2^(SHIFT - 1) or more.
+// A smaller SLACK has sums rescaled more often: 4 prompts of 4096 tokens, 20 heads of 128, SHIFT 6 / 12 / 13 / 14 of an fp16 cache 621 / 620 /
+// 621 / 633 us, 11 / 13 of an int8 cache 662 / 684 (whose values are rounded to 2^-8 of a row's largest anyway).
+template <int DT>
+struct Reference {
+    static constexpr float SHIFT = DT == BRL_I8 ? 11.f : 13.f, SLACK = 15.f - SHIFT;
+};
 
 // fp16 hi and lo of two values, each rounded once (x - hi is exact; the multiply-add rounds it to fp16 directly)
 __device__ __forceinline__ void split_pair(float x0, float x1, uint32_t& hi, uint32_t& lo) {
@@ -410,6 +415,21 @@ __device__ __forceinline__ uint32_t bits_of_group(uint32_t bits, int g) { return
 // where score e of group g stands in its block
 __device__ __forceinline__ constexpr int key_of_score(int g, int e) { return 16 * (e >> 2) + 4 * g + (e & 3); }
 
+// log2 of l 2^ref, as exact as its own size allows (ref is a whole number); +inf where nothing was summed up
+__device__ __forceinline__ float log_sum(float ref, float l) {
+    return l > 0.f ? ref + (float)__builtin_amdgcn_frexp_expf(l) + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l)) : INFINITY;
+}
+
+// int8: what multiplies the codes is a probability times its slot's scale, and scales are of any size.  So the maximum that is followed is
+// that of s + log2(scale) over the slots that the row sees: the products have the bounds that probabilities have otherwise, whatever the
+// scales of slots that the row does not see or hardly weighs.  (Scales count as LEAST_SCALE at least, which keeps the probabilities
+// themselves below 2^90, and parts that meet comparable; values below 1e-25 have fewer digits for it.  Those of values that are no
+// numbers count as that.)
+constexpr float LEAST_SCALE = 0x1p-75f;
+// log2 of x from its bits, at most 0.09 below: exponent and, for the logarithm of a mantissa 1 + f, f
+__device__ __forceinline__ float rough_log2(float x) { return (float)__float_as_uint(x) * 0x1p-23f - 127.f; }
+__device__ __forceinline__ float scale_bits(float x) { return rough_log2(fabsf(x) < INFINITY ? fmaxf(fabsf(x), LEAST_SCALE) : LEAST_SCALE); }
+
 // ---- running softmax and sum of one tile of 16 rows ----
 template <class S>
 struct RowState {
@@ -424,15 +444,29 @@ struct RowState {
 #pragma unroll
         for (int d = 0; d < S::DTL; ++d) o[d] *= f;
     }
-    // s: a lane's scores; on return their probabilities
-    __device__ __forceinline__ void probabilities(float (&s)[8]) {
-        float top = s[0];
+    // s: a lane's scores; on return their probabilities.  scales (int8): of the slots' values.
+    __device__ __forceinline__ void probabilities(float (&s)[8], const float (&scales)[8]) {
+        float top = s[0], most = LEAST_SCALE;
 #pragma unroll
         for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e]);
-        if (__any(top > m + P_SLACK)) {
+        if constexpr (S::DT == BRL_I8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(scales[e]));
+        }
+        // (int8: may be above; the largest scale need not be the likeliest slot's)
+        if (__any((S::DT == BRL_I8 ? top + rough_log2(most) : top) > m + Reference<S::DT>::SLACK)) {
+            if constexpr (S::DT == BRL_I8) {
+                top = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float x = scales[e];
+                    asm volatile("" : "+v"(x));       // (opaque: or this is computed in front of the branch, every time)
+                    top = fmaxf(top, s[e] + scale_bits(x));
+                }
+            }
             top = fmaxf(top, __shfl_xor(top, 16, 64));
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float m_new = fmaxf(m, ceilf(top)), ref_new = m_new == -INFINITY ? 0.f : m_new - P_SHIFT;
+            const float m_new = fmaxf(m, ceilf(top)), ref_new = m_new == -INFINITY ? 0.f : m_new - Reference<S::DT>::SHIFT;
             const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - ref_new);
             l *= alpha;
             scale(alpha);
@@ -718,7 +752,6 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         }
         RowState<S> row;
         row.clear();
-        float unit = 0x1p126f;                                         // int8: power of two that the sums are multiplied by
         const int all_see = st.base + (a.tree ? 0 : 1);                // slots below are seen by every row (causal: by token 0)
         if (threadIdx.x < JOBS) {
             uint4 x, y;
@@ -798,21 +831,11 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
                 reinterpret_cast<float4*>(f)[0] = make_float4(s[0], s[1], s[2], s[3]);
                 reinterpret_cast<float4*>(f)[4] = make_float4(s[4], s[5], s[6], s[7]);
             }
-            row.probabilities(s);
+            row.probabilities(s, vf);
             if (odd) add_strange<S>(a.c, here_lo, here_hi, odd, s, row, at);
             if constexpr (DT == BRL_I8) {
-                // scales relative to the largest so far, a power of two that only falls: fp16 holds the products
-                float top = vf[0];
 #pragma unroll
-                for (int e = 1; e < 8; ++e) top = fmaxf(top, vf[e]);
-                if (__any(top * unit > 1.f)) {
-                    const float now = __builtin_amdgcn_exp2f(-ceilf(__builtin_amdgcn_logf(wave_max(top))) - 1.f);
-                    const float f = now / unit;
-                    row.scale(f);
-                    unit = now;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[e] *= vf[e] * unit;
+                for (int e = 0; e < 8; ++e) s[e] *= vf[e];
             }
             __builtin_amdgcn_wave_barrier();
             block_values<S, 1>(lds, &s, &row, at);
@@ -827,9 +850,8 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
         float top = -INFINITY;
 #pragma unroll 4
         for (int w = 0; w < waves; ++w) top = fmaxf(top, s_ml[w][c].x);
-        float f = row.l > 0.f ? __builtin_amdgcn_exp2f(row.ref - top) : 0.f;
+        const float f = row.l > 0.f ? __builtin_amdgcn_exp2f(row.ref - top) : 0.f;
         if (g == 0) s_l[wave][c] = row.l * f;
-        if constexpr (DT == BRL_I8) f /= unit;
         float* o = reinterpret_cast<float*>(lds);                      // [16 rows][OS]
 #pragma unroll
         for (int d = 0; d < S::DTL; ++d) *reinterpret_cast<v4f*>(o + c * OS + 16 * d + 4 * g) = row.o[d] * f;
@@ -848,7 +870,7 @@ __global__ __launch_bounds__(512, 2) void cached_stream_kernel(CachedAttention a
             }
             if (all) {
                 *reinterpret_cast<v4f*>(out_row(a, st, h, p.group, r) + d) = sum * (l > 0.f ? 1.f / l : 0.f);
-                if (p.lse && d == 0) p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + r] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
+                if (p.lse && d == 0) p.lse[((size_t)b * a.c.n_kv + h) * p.rows_pad + r] = log_sum(ref, l);
             } else {
                 *reinterpret_cast<v4f*>(p.part_o + (slot + r) * DH + d) = sum;
                 if (d == 0) p.part_ml[slot + r] = make_float2(ref, l);
@@ -911,7 +933,7 @@ struct Joiner {
             }
         }
         if (d < DH) *reinterpret_cast<v4f*>(y + d) = o * (l > 0.f ? 1.f / l : 0.f);
-        if (lse && d == 0) *lse = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
+        if (lse && d == 0) *lse = log_sum(ref, l);
     }
 };
 
@@ -1142,7 +1164,6 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
             *reinterpret_cast<uint4*>(s_kv[plane / S::PL] + plane % S::PL * S::PLANE + lds_chunk<S>(key, S::ROW / 8 + x)) = make_uint4(0, 0, 0, 0);
         }
     }
-    float unit_scale;                                                  // int8: power of two that the sums are multiplied by
     // LOOK: strange values are looked for in the blocks with new tokens, which not every row sees.
     auto pass = [&](auto looks) __attribute__((always_inline)) {
         constexpr bool LOOK = decltype(looks)::value;
@@ -1153,7 +1174,6 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
         };
 #pragma unroll
         for (int r = 0; r < RT; ++r) row[r].clear();
-        unit_scale = 0x1p126f;
         store(load[0], first, 0);
         if constexpr (DEPTH == 2) {
             ++ahead;
@@ -1225,7 +1245,7 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
                         }
                     }
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) row[r].probabilities(s[r]);
+                    for (int r = 0; r < RT; ++r) row[r].probabilities(s[r], vf);
                     if (LOOK && has_new(t)) {
                         const uint4 x = s_odd[buf];
                         const uint32_t odd = __builtin_amdgcn_readfirstlane(x.x | x.y | x.z | x.w);
@@ -1235,20 +1255,10 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
                         }
                     }
                     if constexpr (DT == BRL_I8) {
-                        float top = vf[0];
-#pragma unroll
-                        for (int e = 1; e < 8; ++e) top = fmaxf(top, vf[e]);
-                        if (__any(top * unit_scale > 1.f)) {
-                            const float now = __builtin_amdgcn_exp2f(-ceilf(__builtin_amdgcn_logf(wave_max(top))) - 1.f);
-                            const float f = now / unit_scale;
-#pragma unroll
-                            for (int r = 0; r < RT; ++r) row[r].scale(f);
-                            unit_scale = now;
-                        }
 #pragma unroll
                         for (int r = 0; r < RT; ++r)
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) s[r][e] *= vf[e] * unit_scale;
+                            for (int e = 0; e < 8; ++e) s[r][e] *= vf[e];
                     }
                     block_values<S, RT>(vals, s, row, lane);
                 }
@@ -1286,12 +1296,12 @@ __global__ __launch_bounds__(256, 2) void cached_tiles_kernel(CachedAttention a,
         l += __shfl_xor(l, 32, 64);
         const int rr = w0 + r * 16 + c;
         if (rr > r1) continue;
-        float f = DT == BRL_I8 ? 1.f / unit_scale : 1.f;
+        float f = 1.f;
         float* y;
         if (p.splits == 1) {
             f *= l > 0.f ? 1.f / l : 0.f;
             y = out_row(a, st, h, p.group, rr);
-            if (p.lse && g == 0) p.lse[(size_t)unit * p.rows_pad + rr] = l > 0.f ? row[r].ref + __builtin_amdgcn_logf(l) : INFINITY;
+            if (p.lse && g == 0) p.lse[(size_t)unit * p.rows_pad + rr] = log_sum(row[r].ref, l);
         } else {
             const size_t at = ((size_t)unit * p.rows_pad + rr) * p.splits + split;
             y = p.part_o + at * DH;

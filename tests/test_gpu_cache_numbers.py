@@ -3,8 +3,9 @@ behind one dominant key, new rows that are no numbers.
 
 Bounds.  Every (token, head) is judged by its own sum_j p_j |v_j| over the slots that it sees (the largest of its components), never
 by another's.  As in the other cache tests 2e-6 of that for scores of unit scale, and on top what the operands' two fp16 planes do not
-hold: a half step of the smallest fp16 number is 2^-25, and a row's largest probability (int8: its largest product of probability
-and scale) is carried as 2^12 at least, so each probability is off by at most 2^-37 of the largest, the output by 2^-37 sum_j |v_j|.
+hold: a half step of the smallest fp16 number is 2^-25, and a row's largest probability is carried as 2^12 at least, so each probability is off by
+at most 2^-37 of the largest, the output by 2^-37 sum_j |v_j|.  (int8: products of probability and scale, the largest as 2^10 at least, so
+each is off by 2^-35 of the largest, which is a share of the bound below 1e-7 for the few thousand slots here.)
 Values of an fp32 cache are such pairs themselves, taken as they are: off by at most 2^-25 each, and so is their average.
 """
 import numpy as np
@@ -68,7 +69,66 @@ SIZES = [
 
 # ---------------------------------------------------------------- rows of very different size
 
-@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("ratio", [2.0 ** 10, 2.0 ** 31, 2.0 ** 60])
+@pytest.mark.parametrize("mask", ["causal", "tree"])
+@pytest.mark.parametrize("dh,hq,hkv,page,cached,new", SIZES)
+def test_large_int8_rows_stay_with_the_tokens_that_see_them(dh, hq, hkv, page, cached, new, mask, ratio):
+    """New tokens whose value rows are far larger than all others: who does not see them is as exact as without them."""
+    B, R = _mods()
+    print("large rows", dh, hq, hkv, page, cached, new, mask, ratio, flush=True)
+    lens, cu, _, qkv, cos, sin, c, tree = setting(dh, hq, hkv, page, cached, new, mask, "i8", 61)
+    for b, n in enumerate(new):
+        for i in {n // 2, n - 1}:
+            slot = cached[b] + i
+            c["v_scale"][c["table"][b, slot // page], :, slot % page] *= np.float32(ratio)
+    got = OnGpu(B, R, c, dh, cos, sin).attend(qkv, hq, cu, max(new), lens, tree=tree)
+    want, reach = by_head(c, qkv, hq, hkv, dh, cu, lens, None, cos, sin, tree)
+    check_each(got, want, REL * reach)                            # (2^-37 of a few hundred rows: nothing)
+
+
+@pytest.mark.parametrize("new", [1, 33])
+@pytest.mark.parametrize("cached", [100, 3000])
+@pytest.mark.parametrize("slot", [0, 50])
+def test_large_int8_rows_of_no_weight(slot, cached, new):
+    """A value row 2^31 times the others that every token sees, under a key whose probability is 2^-100 and less: in front of the
+    other keys and between them."""
+    B, R = _mods()
+    dh, page = 64, 32
+    lens = [cached + new]
+    cos, sin = tables(lens[0], dh)
+    c = make_cache(63, 1, dh, page, lens, np.int8)
+    qkv = synth.normal(63, new, (new, 3 * dh))
+    qkv[:, :dh] = 1.0                                             # at position 0: no rotation
+    pg, at = c["table"][0, slot // page], slot % page
+    c["k"][pg, 0, at, :dh], c["k_scale"][pg, 0, at] = -127, 12.0 / 127          # score -12 * 64 / 8 = -96, in bits -138
+    c["v_scale"][pg, 0, at] *= np.float32(2.0 ** 31)
+    positions = np.zeros(new, np.int32)
+    got = OnGpu(B, R, c, dh, cos, sin).attend(qkv, 1, None, new, lens, positions=positions)
+    want, reach = by_head(c, qkv, 1, 1, dh, None, lens, positions, cos, sin, None)
+    check_each(got, want, REL * reach)
+
+
+@pytest.mark.parametrize("size", [1e-24, 1e-12, 1.0, 1e4])
+@pytest.mark.parametrize("dh,hq,hkv,page,cached,new", SIZES)
+def test_weights_do_not_follow_the_size_of_int8_values(dh, hq, hkv, page, cached, new, size):
+    """Value rows of any size, and some of zeros between them: the softmax weights are those of the scores."""
+    B, R = _mods()
+    lens, cu, rng, qkv, cos, sin, c, _ = setting(dh, hq, hkv, page, cached, new, "causal", "i8", 71)
+    c["v_scale"] *= np.float32(size)
+    c["v_scale"] = np.where(rng.random(c["v_scale"].shape) < 0.1, np.float32(1e-30) / np.float32(127), c["v_scale"])
+    w = torch.zeros(len(lens), hkv, max(lens), device="cuda")
+    got = OnGpu(B, R, c, dh, cos, sin).attend(qkv, hq, cu, max(new), lens, weights=w)
+    want, added, _ = K.attend(c, qkv, hq, cu, lens, None, cos, sin)
+    g = w.cpu().numpy()
+    assert np.all(np.abs(g - added) <= 4e-6 * added + 2.0 ** -23 * g)
+    want, reach = by_head(c, qkv, hq, hkv, dh, cu, lens, None, cos, sin, None)
+    # values below 1e-23: products with a scale of 2^-86 are carried as 2^(10 + 75 - 86) = 1/2 at least, to 2^-25.  Scales below 2^-75 count
+    # as that, so a token that sees nothing but rows of a scale of 2^-107 (state 2's first token is one, with such a row of codes up to 127) has
+    # its sum of probabilities carried as 2^(10 + 75) at least, each product to 2^-25, codes to 127: off by 127 * 2^-25 * 2^-85 at most.
+    check_each(got, want, (REL + (2.0 ** -23 if size < 1e-20 else 0.0)) * reach + 127 * 2.0 ** -110)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "i8"])
 @pytest.mark.parametrize("mask", ["causal", "tree"])
 @pytest.mark.parametrize("dh,hq,hkv,page,cached,new", SIZES)
 def test_value_rows_of_different_size(dh, hq, hkv, page, cached, new, mask, dtype):
