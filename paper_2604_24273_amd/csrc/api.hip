@@ -1057,7 +1057,7 @@ size_t brl_attention_cached_workspace_bytes(const brl_kv_cache* c, int n_heads, 
     memset(&v, 0, sizeof(v));
     v.n_kv = c->n_kv_heads; v.dh = c->head_dim; v.row = kv_row(c->head_dim); v.dtype = c->dtype;
     v.page_shift = __builtin_ctz((unsigned)c->page_tokens);
-    const size_t need = cached_attention_ws_bytes(v, n_heads, T, B, max_new, max_len, want_weights != 0);
+    const size_t need = cached_attention_ws_bytes(v, n_heads, B, max_new, max_len, want_weights != 0);
     return round_up_sz(need ? need : 1, ALIGN);
 }
 

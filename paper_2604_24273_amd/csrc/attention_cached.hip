@@ -1443,7 +1443,7 @@ struct Layout {
     size_t o_off, ml_off, lse_off, scores_off, q_off, w_off, total;
 };
 
-Layout plan_cached(const KvView& c, int n_heads, int T, int B, int max_new, int max_len, bool weights) {
+Layout plan_cached(const KvView& c, int n_heads, int B, int max_new, int max_len, bool weights) {
     Layout L;
     memset(&L, 0, sizeof(L));
     Plan& p = L.p;
@@ -1593,12 +1593,12 @@ int launch_typed(const CachedAttention& a, const Layout& L, hipStream_t s) {
 
 }  // namespace
 
-size_t cached_attention_ws_bytes(const KvView& c, int n_heads, int T, int B, int max_new, int max_len, bool weights) {
-    return plan_cached(c, n_heads, T, B, max_new, max_len, weights).total;
+size_t cached_attention_ws_bytes(const KvView& c, int n_heads, int B, int max_new, int max_len, bool weights) {
+    return plan_cached(c, n_heads, B, max_new, max_len, weights).total;
 }
 
 int launch_cached_attention(const CachedAttention& a, void* workspace, hipStream_t s) {
-    Layout L = plan_cached(a.c, a.n_heads, a.t.T, a.t.B, a.t.max_new, a.t.max_len, a.weights != nullptr);
+    Layout L = plan_cached(a.c, a.n_heads, a.t.B, a.t.max_new, a.t.max_len, a.weights != nullptr);
     char* base = static_cast<char*>(workspace);
     Plan& p = L.p;
     p.part_o = reinterpret_cast<float*>(base + L.o_off);

@@ -303,7 +303,7 @@ struct CachedAttention {
     float* weights;           // [B, n_kv, ld_weights] or nullptr
     size_t ld_weights;
 };
-size_t cached_attention_ws_bytes(const KvView& c, int n_heads, int T, int B, int max_new, int max_len, bool weights);
+size_t cached_attention_ws_bytes(const KvView& c, int n_heads, int B, int max_new, int max_len, bool weights);
 int launch_cached_attention(const CachedAttention& a, void* workspace, hipStream_t s);
 int launch_cache_select(const float* weights, size_t ld_weights, int B, int n_kv, const int32_t* lens, int max_len, int keep,
                         int first, int recent, int32_t* kept, int32_t* counts, hipStream_t s);

@@ -154,7 +154,7 @@ int append_typed(AppendArgs a, hipStream_t s) {
 // One workgroup per list.  The threshold (the key of the last slot that is taken) is found bit group by bit group: a histogram
 // of the next bits of the keys that agree with the threshold so far, scanned from the top.  Then one pass in slot order takes
 // what lies above it and the first of those equal to it.
-constexpr int SEL_THREADS = 1024, SEL_BINS = 2048, SEL_COPIES = 8, PARTS = SEL_THREADS / 64;
+constexpr int SEL_THREADS = 1024, SEL_BINS = 2048, PARTS = SEL_THREADS / 64;
 
 struct SelectArgs {
     const float* weights;
