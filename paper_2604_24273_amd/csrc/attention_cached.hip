@@ -1452,20 +1452,24 @@ Layout plan_cached(const KvView& c, int n_heads, int B, int max_new, int max_len
     p.rows_max = max_new * p.group.n;
     p.splits = 1;
     const int units = B * c.n_kv, blocks = (max_len + 31) / 32;
-    // 16 rows fill one column block of the matrix instructions; more would have a wavefront of the first form hold two.  20 rows, 64
-    // states of 1000-2000 slots, first form / second: fp16 82 / 75 us, fp32 175 / 123; 4 rows: 80 / 93 and 142 / 155.
+    // 16 rows fill one column block of the matrix instructions; more would have a wavefront of the first form hold two.  64 states of 1000-2000
+    // slots, 5 heads of 128, first form / second, us: 4 rows fp32 105 / 114, fp16 58 / 71, int8 41 / 62; 16 rows 117 / 120, 70 / 75, 51 / 64.
     L.tiles = p.rows_max > 16;
     size_t parts;
     if (!L.tiles) {
         p.rows_pad = 16;
         // A workgroup per (state, k/v head) needs no second launch (about 7 us) but takes all of a state's keys through one compute unit:
         // up to two turns of its eight wavefronts of an fp32 cache, four of the others, which are half the work, twice that
-        // where there are workgroups to fill every unit.  5 heads of 128 and 1000 slots, this form / shared: fp16 14.0 / 13.8 us,
-        // fp32 23.0 / 17.2, 512 slots 12.2 / 18.6 and 19.5 / 23.1; 1280 of 1000: fp16 116 / 126; 5 of 2000: 18.4 / 13.8.
+        // where there are workgroups to fill every unit.  Heads of 128, this form / shared, us, fp32, fp16 and int8: 5 of 300 slots 16.2 / 20.8,
+        // 10.3 / 16.2, 10.4 / 17.3; 5 of 500 19.3 / 15.0, 11.5 / 12.4, 11.4 / 12.8; 5 of 1000 29.0 / 15.1, 16.5 / 12.3, 15.0 / 12.9; 255 of 1000
+        // 52 / 58, 28.3 / 33.4, 18.3 / 23.3; 320 of 1000 76 / 72, 40 / 43, 25 / 30; 550 of 1800 204 / 193, 105 / 108, 71 / 74.
         const int whole = c.dtype == BRL_F32 ? 16 : 32;
         if (blocks <= whole || (units >= 512 && blocks <= 64) || (long long)units * p.rows_max > (1 << 22) ||
             (long long)units * blocks >= (1ll << 31)) {
-            L.waves = blocks <= 4 || units >= 2048 ? 4 : 8;
+            // Eight wavefronts where a workgroup has a compute unit to itself and blocks for them, else four, so that two workgroups share
+            // a unit.  4 / 8, us: 5 of 120 slots fp32 11.0 / 15.4, fp16 8.9 / 9.5; 5 of 1000 int8 17.7 / 15.0; 255 of 1800 fp32 89 / 85, fp16 47 / 45,
+            // int8 31 / 28; 320 of 300 fp16 16.3 / 22.1, of 1000 40 / 45; 1280 of 300 fp32 82 / 105, fp16 47 / 63; 4000 of 1000 355 / 379.
+            L.waves = blocks <= 4 || units > 256 ? 4 : 8;
         } else {
             L.waves = 4;
             p.groups = 512;                           // as many as run at a time
@@ -1481,7 +1485,10 @@ Layout plan_cached(const KvView& c, int n_heads, int B, int max_new, int max_len
         const int new_blocks = (max_new + 31) / 32, most = blocks / 8 < 64 ? blocks / 8 : 64;
         if (4 * new_blocks < blocks) {
             // Long keys.  A workgroup costs its blocks and about four more (queries, first loads, end), parts that have to be joined another
-            // four; the split with the shortest sum of rounds.
+            // four; the split with the shortest sum of rounds.  This / the other rule's number of parts, heads of 128, fp16 and fp32, us: 80
+            // workgroups (8 x 48 tokens on 2000 slots) 44 / 57 and 60 / 73; 140 (4 x 200 on 2000) 67 / 78 and 91 / 108; 190 (38 x 7 on 5000) 121 /
+            // 113 and 199 / 243; 320 (64 x 7 on 2000) 89 / 83 and 147 / 130, int8 77 / 90; 640 (128 x 7 on 5000) 351 / 315 and 620 / 684, int8 288 / 353.
+            // With a quarter of the slots new and more, or few workgroups, both rules choose alike or nearly so.
             long long best = 0;
             for (int s = 1; s == 1 || s <= most; ++s) {
                 const long long cost = (groups * s + 511) / 512 * ((blocks + s - 1) / s + 4) + (s > 1 ? 4 + s / 8 : 0);
@@ -1492,7 +1499,7 @@ Layout plan_cached(const KvView& c, int n_heads, int B, int max_new, int max_len
             // to be joined: only until all units have work.  1 / 2 / 3 / 4 parts, us: 650 workgroups (2 x 2000 tokens, 5 groups of 4 heads of
             // 128, fp16) 115 / 144 / 171 / 184; 640 205 / 225 / 250 / 251; 512 (heads of 100) 105 / 128 / 139 / 152; 256 (fp32) 80 / 68 /
             // 80 / 85; 235 (fp32) 107 / 84 / 81 / 90; 136 (heads of 64) 64 / 46 / 39 / 37.  160 (1 x 1000, fp16): 44 with 3, 54 with 4; 188 (heads
-            // of 16): 39 with 2, 32 with 3.
+            // of 16): 39 with 2, 32 with 3.  320 (2 x 1000): fp16 56 / 62 / 74 / 88, fp32 81 / 71 / 87 / 101.
             const long long s = 576 / groups;
             p.splits = s < 1 || most < 1 ? 1 : s < most ? (int)s : most;
         }
