@@ -360,10 +360,14 @@ int attention_forward(const float* qkv, int B, int S,
  *   page_table       DEVICE [B, table_pages] int32: slot j of state b is row
  *                    j % page_tokens of page page_table[b, j / page_tokens]
  * (n_pages * n_kv_heads * page_tokens below 2^31.)
- * dtype BRL_F32 (attention as exact as attention_forward's), BRL_F16 or BRL_I8.
+ * dtype BRL_F32 (attention as exact as attention_forward's with BRL_ATTN_MFMA; there
+ * is no form on the vector ALUs), BRL_F16 or BRL_I8.
  * The struct is read on the HOST during the call.  Which pages a state owns
  * is the caller's business; pages may be shared between states as long as
- * nobody writes them.  Slots at lens[b] and behind are never read.
+ * nobody writes them.  What is in slots at lens[b] and behind, and in pages that no
+ * state owns, has no part in any result, but kernels load whole pieces of 16 rows
+ * and, for slots that are not there, the first rows of the pool: all of k, v and
+ * the scales must be readable memory.
  *
  * New tokens: qkv [T, (n_heads + 2 n_kv_heads) * head_dim] fp32 rows as in
  * attention_forward.  State b owns rows cu_new[b] .. cu_new[b+1]-1 (DEVICE [B+1]
@@ -381,6 +385,10 @@ int attention_forward(const float* qkv, int B, int S,
  * moved), a token that has no slot (more new tokens than lens) sees no key
  * before slot 0 and is not stored.
  * All calls only enqueue kernels and can be captured into a HIP graph.
+ * A call repeated gives the same bits.  The last bits of a state's attention may
+ * depend on the other states of the call and on its bounds (T, B, max_new, max_len),
+ * which decide how the keys are cut into parts - unlike encoder_forward's states,
+ * which do not depend on their batch.
  * BRL_EINVAL where one call would be too much: B n_heads above 2^22, max_new
  * n_heads B above 2^26, max_new times the square of the heads per k/v head from
  * 2^32 on, B n_kv_heads max_len above 2^30 with weights, B n_kv_heads above 2^21
